@@ -13,7 +13,11 @@
  * pv_codebook_grads (Alg. 3 P step: gradients of codebooks and scales),
  * pv_dequantize_groups (dequantisation of the re-encoded groups only),
  * pv_select_topk_groups_noalloc (the selection for callers that cannot allocate),
- * pv_dequantize_scalar / pv_reencode_scalar (App. K's scalar uniform-grid representation).
+ * pv_dequantize_scalar / pv_reencode_scalar (App. K's scalar uniform-grid representation),
+ * pv_quantize_mx / pv_dequantize_mx (weights and activations in 4 or 8 bits whose blocks share a
+ * power of two), pv_mx_product[_grads] (the product with such weights, and its gradients),
+ * pv_rms_norm[_backward] (which hands its output over in 8 bits), pv_distill_topk[_backward]
+ * (the loss of App. K's fine-tuning: distillation from a teacher, here from its top logits).
  * Instrumentation: pv_set_search_mode, pv_timing_*, pv_reencode_stats, and the two ceiling
  * probes pv_probe_copy / pv_probe_mfma_f16.
  *
@@ -281,6 +285,120 @@ pv_status pv_reencode_scalar(pv_ctx *ctx, int64_t out_features, int64_t in_featu
                              const float *zeros, const int32_t *weight_idx, int64_t k,
                              uint8_t *codes, int64_t *num_changed /* NULL ok */);
 
+/* ---- microscaled representation: 32 consecutive values of a row share a power of two ----
+ * The matrix cores of gfx950 multiply it as it is stored.  A matrix [rows, cols] has
+ * nblk = ceil(cols / 32) blocks a row:
+ *   scales  u8 [rows, nblk]: E + 127, the block's power of two 2^E; 255: every value of the block is NaN
+ *   codes   PV_MX_E2M1: u8 [rows, nblk * 16], element 2i in the low four bits of byte i, sign | 2
+ *           exponent bits | 1 mantissa bit: 0 0.5 1 1.5 2 3 4 6;
+ *           PV_MX_E4M3: u8 [rows, nblk * 32], sign | 4 | 3, largest 448, 0x7f and 0xff are NaN
+ * and stands for code * 2^E.  Elements behind `cols` in a row's last block are zero codes: the
+ * quantisation writes them, the product relies on them.
+ * Tensors of the calls below are row-major and dense, except that logits have a row stride.
+ * Rows need no alignment of their own (any cols).  rows, cols: 0 <= cols < 2^31 - 1024 and
+ * rows * ceil(cols / 32) * 32 < 2^46, so offsets are held in 64 bits. */
+typedef enum {
+    PV_F32 = 0,
+    PV_BF16 = 1,
+    PV_F16 = 2
+} pv_dtype;
+
+typedef enum {
+    PV_MX_E2M1 = 0, /* 4 bits, E = floor(log2(max |x|)) - 2 */
+    PV_MX_E4M3 = 1  /* 8 bits, E = floor(log2(max |x|)) - 8 */
+} pv_mx_format;
+
+/* X [rows, cols] of type x_type to codes and scales.  E as above, clamped to [-127, 127] (a
+ * block of zeros has E = -127); each code is the value of the format nearest to x * 2^-E, ties to
+ * the even code, values beyond the largest one become it.  A block with a NaN or an infinity gets
+ * the scale 255 and zero codes.  This is the V step on this representation for targets X (every
+ * weight rounded to its block's grid) and the preparation of activations for pv_mx_product. */
+pv_status pv_quantize_mx(pv_ctx *ctx, int64_t rows, int64_t cols, pv_mx_format format,
+                         pv_dtype x_type, const void *X, uint8_t *codes, uint8_t *scales);
+
+/* out [rows, cols] = the values that codes and scales stand for, rounded once to out_type (exact
+ * in f32; exact in bf16 unless below its normal range). */
+pv_status pv_dequantize_mx(pv_ctx *ctx, int64_t rows, int64_t cols, pv_mx_format format,
+                           const uint8_t *codes, const uint8_t *scales, pv_dtype out_type,
+                           void *out);
+
+/* Y [tokens, out_features] = X W^T, both microscaled along in_features: X in x_format, W
+ * [out_features, in_features] in PV_MX_E2M1.  Sums in fp32, rounded once to y_type.
+ * Y in bf16 or f16, and any Y of X in E2M1: the scaled matrix instruction on the codes.  It cuts
+ * products of E4M3 13 bits below the largest of 16 before it adds them (about 5e-6 of a sum of
+ * normal data).  Y in f32 of X in E4M3: X and W take part as bf16, at half the rate, and nothing
+ * is cut; bf16 holds every value of a code and a scale in [2^-117, 2^119] exactly, and the
+ * quantisation makes no larger one.  in_features == 0 gives zeros. */
+pv_status pv_mx_product(pv_ctx *ctx, int64_t tokens, int64_t out_features, int64_t in_features,
+                        pv_mx_format x_format, const uint8_t *x_codes, const uint8_t *x_scales,
+                        const uint8_t *w_codes, const uint8_t *w_scales, pv_dtype y_type, void *Y);
+
+/* The gradients of that product for dY bf16 [tokens, out_features], taken through the
+ * quantisation unchanged (straight through):
+ *   dX [tokens, in_features] of type dx_type = dY W           NULL ok
+ *   dW f32 [out_features, in_features]       = dY^T X         NULL ok; the G of pv_encode_targets
+ * W and X take part as bf16 (see above); sums in fp32.  The operands of a gradient that is not asked for are not read and may be
+ * NULL (X for dX alone, W for dW alone).  The outputs are overwritten.  Scratch of the context:
+ * W, X and dY transposed in bf16. */
+pv_status pv_mx_product_grads(pv_ctx *ctx, int64_t tokens, int64_t out_features,
+                              int64_t in_features, pv_mx_format x_format, const uint8_t *x_codes,
+                              const uint8_t *x_scales, const uint8_t *w_codes,
+                              const uint8_t *w_scales, const void *dY /* bf16 */,
+                              pv_dtype dx_type, void *dX /* NULL ok */, float *dW /* NULL ok */);
+
+/* Root-mean-square norm with the residual's addition, per row of [rows, cols]:
+ *   h = x + residual          rounded to `type` (residual NULL: h = x)
+ *   rstd = (sum_i h_i^2 / cols + eps)^(-1/2)      f32, sum in f32, of the ROUNDED h
+ *   y_i = (h_i * rstd) * weight_i                 f32
+ * x, residual, h, y of `type`; weight f32 [cols].  Outputs, each NULL ok, at least one of them
+ * given: h; y rounded to `type`; codes and scales, both or neither: y (not rounded to `type`
+ * before) as pv_quantize_mx with `format`; rstd f32 [rows], which the backward call takes.
+ * h may be x or residual, y may be x or residual (exactly the same pointer), h and y differ. */
+pv_status pv_rms_norm(pv_ctx *ctx, int64_t rows, int64_t cols, pv_dtype type, const void *x,
+                      const void *residual /* NULL ok */, const float *weight, float eps, void *h,
+                      void *y, pv_mx_format format, uint8_t *codes, uint8_t *scales, float *rstd);
+
+/* Its gradients, with n_i = h_i * rstd:
+ *   dx_i = dh_i + rstd * (dy_i weight_i - n_i * sum_j(dy_j weight_j n_j) / cols)
+ *   dweight_i = sum over rows of dy_i n_i         f32 [cols], in an order that only rows and cols fix
+ * dx (of `type`) is the gradient of x and of residual alike; dh (NULL: zero) is what arrives at h
+ * from the layers behind.  dx, dweight: each NULL ok, not both.  dx may be dy, dh or h (exactly the
+ * same pointer).  rows == 0: dweight is zero. */
+pv_status pv_rms_norm_backward(pv_ctx *ctx, int64_t rows, int64_t cols, pv_dtype type,
+                               const void *dy, const void *dh /* NULL ok */, const void *h,
+                               const float *weight, const float *rstd, void *dx, float *dweight);
+
+/* Distillation from a teacher's top logits (App. K trains on the divergence from the teacher;
+ * a teacher's k largest logits a token are what is kept of it).  Per row, with t = temperature,
+ * z the logits, (id_j, u_j) the teacher's entries (an id outside [0, vocab) is no entry):
+ *   p = softmax over the entries of u_j / t      q = softmax over the vocabulary of z_v / t
+ *   loss = row_weight * t^2 * sum_j p_j (ln p_j - ln q[id_j])                     f32 [rows]
+ *   lse  = ln sum_v exp(z_v / t)                                                  f32 [rows], NULL ok
+ *   grad_v = row_weight * t * (q_v - sum over j with id_j == v of p_j)            NULL ok
+ * i.e. grad is the gradient of the loss by z_v, in the logits' type; an id that appears twice
+ * counts twice.  row_weight f32 [rows] (NULL: 1): a row of weight 0 is not read; its loss, lse and
+ * gradient are 0.  A row without an entry, or whose entries are all -infinity, has loss 0 and
+ * gradient 0 (lse is still written).  An entry with p_j == 0 adds nothing whatever q is there.
+ * logits [rows, vocab], row stride ld >= vocab elements; grad alike with grad_ld, and may be logits
+ * (same pointer and stride): behind a row's vocab elements nothing is read or written.
+ * teacher_ids i32 [rows, k], teacher_logits f32 [rows, k].  0 <= k <= 1024, 1 <= vocab <= 2^20,
+ * temperature > 0. */
+pv_status pv_distill_topk(pv_ctx *ctx, int64_t rows, int64_t vocab, int32_t k, pv_dtype type,
+                          const void *logits, int64_t ld, const int32_t *teacher_ids,
+                          const float *teacher_logits, float temperature,
+                          const float *row_weight /* NULL ok */, float *loss, float *lse,
+                          void *grad, int64_t grad_ld);
+
+/* The gradient alone, of a forward call without row_weight, for d phi / d loss given afterwards:
+ *   grad_v = grad_loss * t * (q_v - sum over j with id_j == v of p_j),  q_v = exp(z_v / t - lse)
+ * lse f32 [rows] as pv_distill_topk wrote it; grad_loss f32 [rows]: a row of 0 is not read, its
+ * gradient is 0. */
+pv_status pv_distill_topk_backward(pv_ctx *ctx, int64_t rows, int64_t vocab, int32_t k,
+                                   pv_dtype type, const void *logits, int64_t ld,
+                                   const int32_t *teacher_ids, const float *teacher_logits,
+                                   float temperature, const float *lse, const float *grad_loss,
+                                   void *grad, int64_t grad_ld);
+
 /* ---- instrumentation (does not change results) ------------------------- */
 
 /* Search strategy: 0 = automatic (a matrix-core filter with exact certificates
@@ -303,7 +421,11 @@ typedef enum {
     PV_K_PROBE_COPY = 11, /* pv_probe_copy                                                 */
     PV_K_PROBE_MFMA = 12, /* pv_probe_mfma_f16                                             */
     PV_K_STOCHASTIC = 13, /* pv_reencode_groups_stochastic                                 */
-    PV_K_COUNT = 14
+    PV_K_MX_CONVERT = 14, /* pv_quantize_mx, pv_dequantize_mx                              */
+    PV_K_MX_PRODUCT = 15, /* all kernels of pv_mx_product and pv_mx_product_grads          */
+    PV_K_RMS_NORM = 16,   /* pv_rms_norm, pv_rms_norm_backward                             */
+    PV_K_DISTILL = 17,    /* pv_distill_topk, pv_distill_topk_backward                     */
+    PV_K_COUNT = 18
 } pv_kernel_id;
 
 /* With timing on, each kernel (group) above is bracketed by HIP events on the

@@ -21,7 +21,13 @@ KERNEL_IDS = {
     "encode_targets": 0, "group_scores": 1, "select": 2, "prep": 3, "score_mfma": 4,
     "rerank": 5, "exact_scan": 6, "beam": 7, "dequantize": 8, "trust_ratio": 9, "pstep": 10, "stochastic": 13,
     "probe_copy": 11, "probe_mfma": 12,
+    "mx_convert": 14, "mx_product": 15, "rms_norm": 16, "distill": 17,
 }
+
+# pv_mx_format and pv_dtype
+MX_FORMATS = {"e2m1": 0, "e4m3": 1}
+MX_BLOCK = 32
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 class PVError(RuntimeError):
@@ -100,6 +106,14 @@ def load_library():
     lib.pv_reencode_stats.argtypes = [vp, ctypes.POINTER(i64)]
     lib.pv_probe_copy.argtypes = [vp, vp, vp, i64]
     lib.pv_probe_mfma_f16.argtypes = [vp, i64, vp, ctypes.POINTER(i64)]
+    lib.pv_quantize_mx.argtypes = [vp, i64, i64, i32, i32, vp, vp, vp]
+    lib.pv_dequantize_mx.argtypes = [vp, i64, i64, i32, vp, vp, i32, vp]
+    lib.pv_mx_product.argtypes = [vp, i64, i64, i64, i32, vp, vp, vp, vp, i32, vp]
+    lib.pv_mx_product_grads.argtypes = [vp, i64, i64, i64, i32, vp, vp, vp, vp, vp, i32, vp, vp]
+    lib.pv_rms_norm.argtypes = [vp, i64, i64, i32, vp, vp, vp, f32, vp, vp, i32, vp, vp, vp]
+    lib.pv_rms_norm_backward.argtypes = [vp, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp]
+    lib.pv_distill_topk.argtypes = [vp, i64, i64, i32, i32, vp, i64, vp, vp, f32, vp, vp, vp, vp, i64]
+    lib.pv_distill_topk_backward.argtypes = [vp, i64, i64, i32, i32, vp, i64, vp, vp, f32, vp, vp, vp, i64]
     for name in ("pv_create", "pv_select_topk_groups_noalloc", "pv_encode_targets", "pv_encode_targets_adam", "pv_select_topk_groups",
                  "pv_encode_targets_adam_select",
                  "pv_encode_targets_select", "pv_reencode_groups", "pv_reencode_groups_stochastic",
@@ -107,7 +121,9 @@ def load_library():
                  "pv_codebook_grads", "pv_dequantize_scalar", "pv_reencode_scalar",
                  "pv_dequantize_groups",
                  "pv_dequantize", "pv_set_search_mode", "pv_timing_enable", "pv_timing_reset",
-                 "pv_timing_read", "pv_reencode_stats", "pv_probe_copy", "pv_probe_mfma_f16"):
+                 "pv_timing_read", "pv_reencode_stats", "pv_probe_copy", "pv_probe_mfma_f16",
+                 "pv_quantize_mx", "pv_dequantize_mx", "pv_mx_product", "pv_mx_product_grads",
+                 "pv_rms_norm", "pv_rms_norm_backward", "pv_distill_topk", "pv_distill_topk_backward"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -125,6 +141,18 @@ def _dev_ptr(t, dtype, what: str, allow_none: bool = False):
     if not t.is_contiguous():
         raise TypeError(f"{what} must be contiguous")
     return t.data_ptr()
+
+
+def _mx_format(fmt) -> int:
+    if fmt not in MX_FORMATS:
+        raise ValueError(f"format must be one of {sorted(MX_FORMATS)}, got {fmt!r}")
+    return MX_FORMATS[fmt]
+
+
+def mx_shapes(rows: int, cols: int, fmt: str):
+    """Shapes of the codes and the scales (both uint8) of a [rows, cols] matrix."""
+    nblk = -(-cols // MX_BLOCK)
+    return (rows, nblk * (MX_BLOCK // 2 if _mx_format(fmt) == 0 else MX_BLOCK)), (rows, nblk)
 
 
 class PVContext:
@@ -285,6 +313,117 @@ class PVContext:
             self._h, ctypes.byref(lay), _dev_ptr(codes, torch.uint16, "codes"),
             _dev_ptr(codebooks, torch.float32, "codebooks"),
             _dev_ptr(scales, torch.float32, "scales"), _dev_ptr(W_out, torch.float32, "W_out")))
+
+    # ---- operators around the V step --------------------------------------
+    def _tensor(self, t, dtype, shape, what: str, allow_none: bool = False):
+        """Address of a dense tensor of this device, type(s) and shape."""
+        if t is None and allow_none:
+            return None
+        types = dtype if isinstance(dtype, tuple) else (dtype,)
+        if isinstance(t, torch.Tensor) and t.dtype not in types:
+            raise TypeError(f"{what} must be {' or '.join(map(str, types))}, got {t.dtype}")
+        ptr = _dev_ptr(t, getattr(t, "dtype", None), what)
+        if t.device.index != self.device:
+            raise ValueError(f"{what} is on {t.device}, the context on device {self.device}")
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{what} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
+        return ptr
+
+    def _coded(self, rows: int, cols: int, fmt: str, codes, scales, what: str = "", allow_none: bool = False):
+        shapes = mx_shapes(rows, cols, fmt)
+        return [self._tensor(t, torch.uint8, s, what + n, allow_none)
+                for t, s, n in ((codes, shapes[0], "codes"), (scales, shapes[1], "scales"))]
+
+    def pv_quantize_mx(self, rows: int, cols: int, fmt: str, X, codes, scales):
+        x = self._tensor(X, tuple(_DTYPES), (rows, cols), "X")
+        self._check(self._lib.pv_quantize_mx(self._h, int(rows), int(cols), _mx_format(fmt), _DTYPES[X.dtype], x,
+                                             *self._coded(rows, cols, fmt, codes, scales)))
+
+    def pv_dequantize_mx(self, rows: int, cols: int, fmt: str, codes, scales, out):
+        o = self._tensor(out, tuple(_DTYPES), (rows, cols), "out")
+        self._check(self._lib.pv_dequantize_mx(self._h, int(rows), int(cols), _mx_format(fmt),
+                                               *self._coded(rows, cols, fmt, codes, scales), _DTYPES[out.dtype], o))
+
+    def pv_mx_product(self, tokens: int, out_features: int, in_features: int, x_format: str, x_codes, x_scales,
+                      w_codes, w_scales, Y):
+        y = self._tensor(Y, tuple(_DTYPES), (tokens, out_features), "Y")
+        self._check(self._lib.pv_mx_product(
+            self._h, int(tokens), int(out_features), int(in_features), _mx_format(x_format),
+            *self._coded(tokens, in_features, x_format, x_codes, x_scales, "x_"),
+            *self._coded(out_features, in_features, "e2m1", w_codes, w_scales, "w_"), _DTYPES[Y.dtype], y))
+
+    def pv_mx_product_grads(self, tokens: int, out_features: int, in_features: int, x_format: str, x_codes, x_scales,
+                            w_codes, w_scales, dY, dX=None, dW=None):
+        dx = self._tensor(dX, tuple(_DTYPES), (tokens, in_features), "dX", allow_none=True)
+        self._check(self._lib.pv_mx_product_grads(
+            self._h, int(tokens), int(out_features), int(in_features), _mx_format(x_format),
+            *self._coded(tokens, in_features, x_format, x_codes, x_scales, "x_", allow_none=dW is None),
+            *self._coded(out_features, in_features, "e2m1", w_codes, w_scales, "w_", allow_none=dX is None),
+            self._tensor(dY, torch.bfloat16, (tokens, out_features), "dY"),
+            _DTYPES[dX.dtype] if dX is not None else 0, dx,
+            self._tensor(dW, torch.float32, (out_features, in_features), "dW", allow_none=True)))
+
+    def pv_rms_norm(self, rows: int, cols: int, x, residual, weight, eps: float, h=None, y=None, fmt: str = "e4m3",
+                    codes=None, scales=None, rstd=None):
+        xp = self._tensor(x, tuple(_DTYPES), (rows, cols), "x")
+        same = lambda t, what: self._tensor(t, x.dtype, (rows, cols), what, allow_none=True)  # noqa: E731
+        c, s = self._coded(rows, cols, fmt, codes, scales, allow_none=True)
+        self._check(self._lib.pv_rms_norm(
+            self._h, int(rows), int(cols), _DTYPES[x.dtype], xp, same(residual, "residual"),
+            self._tensor(weight, torch.float32, (cols,), "weight"), float(eps), same(h, "h"), same(y, "y"),
+            _mx_format(fmt), c, s, self._tensor(rstd, torch.float32, (rows,), "rstd", allow_none=True)))
+
+    def pv_rms_norm_backward(self, rows: int, cols: int, dy, dh, h, weight, rstd, dx=None, dweight=None):
+        g = self._tensor(dy, tuple(_DTYPES), (rows, cols), "dy")
+        same = lambda t, what, none: self._tensor(t, dy.dtype, (rows, cols), what, allow_none=none)  # noqa: E731
+        self._check(self._lib.pv_rms_norm_backward(
+            self._h, int(rows), int(cols), _DTYPES[dy.dtype], g, same(dh, "dh", True), same(h, "h", False),
+            self._tensor(weight, torch.float32, (cols,), "weight"), self._tensor(rstd, torch.float32, (rows,), "rstd"),
+            same(dx, "dx", True), self._tensor(dweight, torch.float32, (cols,), "dweight", allow_none=True)))
+
+    def _strided(self, t, dtype, rows: int, vocab: int, what: str):
+        """Address and row stride of [rows, vocab] whose rows are dense."""
+        if t is None:
+            return None, vocab
+        types = dtype if isinstance(dtype, tuple) else (dtype,)
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in types:
+            raise TypeError(f"{what} must be a CUDA tensor of {' or '.join(map(str, types))}")
+        if t.device.index != self.device:
+            raise ValueError(f"{what} is on {t.device}, the context on device {self.device}")
+        if tuple(t.shape) != (rows, vocab):
+            raise ValueError(f"{what} must have the shape {(rows, vocab)}, got {tuple(t.shape)}")
+        ld = t.stride(0) if rows > 1 else vocab
+        if (vocab > 1 and t.stride(1) != 1) or ld < vocab:
+            raise TypeError(f"{what} must have dense rows that do not overlap, got strides {t.stride()}")
+        return t.data_ptr(), ld
+
+    def _teacher(self, rows: int, k: int, ids, logits):
+        return (self._tensor(ids, torch.int32, (rows, k), "teacher_ids", allow_none=(k == 0)),
+                self._tensor(logits, torch.float32, (rows, k), "teacher_logits", allow_none=(k == 0)))
+
+    def pv_distill_topk(self, rows: int, vocab: int, k: int, logits, teacher_ids, teacher_logits, temperature: float,
+                        row_weight=None, loss=None, lse=None, grad=None):
+        row = lambda t, what, none: self._tensor(t, torch.float32, (rows,), what, allow_none=none)  # noqa: E731
+        if logits is None:
+            raise TypeError("logits is None")
+        z, ld = self._strided(logits, tuple(_DTYPES), rows, vocab, "logits")
+        g, grad_ld = self._strided(grad, logits.dtype, rows, vocab, "grad")
+        ids, top = self._teacher(rows, k, teacher_ids, teacher_logits)
+        self._check(self._lib.pv_distill_topk(
+            self._h, int(rows), int(vocab), int(k), _DTYPES[logits.dtype], z, ld, ids, top, float(temperature),
+            row(row_weight, "row_weight", True), row(loss, "loss", False), row(lse, "lse", True), g, grad_ld))
+
+    def pv_distill_topk_backward(self, rows: int, vocab: int, k: int, logits, teacher_ids, teacher_logits,
+                                 temperature: float, lse, grad_loss, grad):
+        row = lambda t, what: self._tensor(t, torch.float32, (rows,), what)  # noqa: E731
+        if logits is None or grad is None:
+            raise TypeError("logits or grad is None")
+        z, ld = self._strided(logits, tuple(_DTYPES), rows, vocab, "logits")
+        g, grad_ld = self._strided(grad, logits.dtype, rows, vocab, "grad")
+        ids, top = self._teacher(rows, k, teacher_ids, teacher_logits)
+        self._check(self._lib.pv_distill_topk_backward(
+            self._h, int(rows), int(vocab), int(k), _DTYPES[logits.dtype], z, ld, ids, top, float(temperature),
+            row(lse, "lse"), row(grad_loss, "grad_loss"), g, grad_ld))
 
     # ---- instrumentation --------------------------------------------------
     def pv_set_search_mode(self, mode: int):

@@ -163,9 +163,14 @@ extern "C" void pv_destroy(pv_ctx *c)
     if (!c) return;
     (void)hipSetDevice(c->device);
     (void)hipStreamSynchronize(c->stream);
-    pv_buffer *bufs[] = {&c->select, &c->sample, &c->stats, &c->search, &c->fb_list, &c->trust, &c->pstep};
+    pv_buffer *bufs[] = {&c->select, &c->sample, &c->stats, &c->search, &c->fb_list, &c->trust, &c->pstep, &c->ops};
     for (pv_buffer *b : bufs)
         if (b->ptr) (void)hipFree(b->ptr);
+    while (pv_retired *r = c->retired) {
+        c->retired = r->next;
+        (void)hipFree(r->ptr);
+        delete r;
+    }
     for (auto &t : c->timers)
         for (hipEvent_t e : t.pending) (void)hipEventDestroy(e);
     for (hipEvent_t e : c->event_pool) (void)hipEventDestroy(e);

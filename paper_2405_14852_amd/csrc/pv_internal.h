@@ -24,6 +24,12 @@ struct pv_timer {
     int64_t launches = 0;
 };
 
+// a block of scratch that captured graphs may still use
+struct pv_retired {
+    void *ptr;
+    pv_retired *next;
+};
+
 struct pv_ctx {
     int device = 0;
     hipStream_t stream = nullptr;
@@ -46,6 +52,9 @@ struct pv_ctx {
     const uint32_t *rr_counts = nullptr;  // in there: [blocks][4] counters of the last call's re-rank kernel
     pv_buffer fb_list;      // beam path: the groups left to the exact kernel
     pv_buffer trust;        // scratch of the trust-ratio call (saved codes, keys, prefix sums, sort space)
+    pv_buffer ops;          // scratch of the operators around the V step (see pv_ops_scratch)
+    bool ops_captured = false;            // a captured call has used it: it is not freed when it is replaced
+    pv_retired *retired = nullptr;        // and those that were
     pv_buffer pstep;        // scratch of the P-step gradients (tiles in bucket order and where their buckets start, sums that go on; or the blocks' tables)
 };
 
