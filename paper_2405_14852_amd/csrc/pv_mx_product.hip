@@ -176,6 +176,249 @@ __global__ __launch_bounds__(256) void k_product_direct(operand w, operand x, in
     }
 }
 
+// ---------------------------------------------------------------- tiles through LDS
+
+// A step is 128 values of a microscaled row or 64 of a bf16 one: `bytes` of it, in pieces of 16.
+template <int KIND>
+struct step_of {
+    static constexpr int bytes = KIND == kE2M1 ? 64 : 128, pieces = bytes / 16;
+    static constexpr int values = KIND == kBF16 ? 64 : 128, blocks = values / 32;
+};
+
+// Where piece c of a tile's row lies in LDS: rows are `bytes` apart, and the pieces of a row change places by a key
+// of the row, so that the eight lanes that read at a time - rows 8 a + 0 .. 3 and 8 a + 8 .. 11 of a pair of fragments, the same
+// piece - meet 32 different banks.
+template <int KIND>
+__device__ __forceinline__ int key_of(int row)
+{
+    if constexpr (step_of<KIND>::pieces == 8) return (row & 3) | (row >> 3 & 1) << 2;
+    return (row >> 1 & 1) | (row >> 3 & 1) << 1;
+}
+
+// BYTES (16 or 4) a lane from memory to LDS, lane i to `to` + BYTES * i
+template <int BYTES>
+__device__ __forceinline__ void fetch(const void *from, unsigned to)
+{
+    const auto at = (__attribute__((address_space(3))) void *)(uintptr_t)to;
+    if constexpr (BYTES == 16) __builtin_amdgcn_global_load_lds(from, at, 16, 0, 0);
+    else __builtin_amdgcn_global_load_lds(from, at, 4, 0, 0);
+}
+
+// All but the last N memory operations of this wave are done, and every wave has come here.
+template <int N>
+__device__ __forceinline__ void wait_and_meet()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+struct tiling {
+    int nblk;                // blocks of 32 values a row
+    int wtiles, xtiles;
+    int splits;              // of the steps
+    int64_t scale_pitch;     // bytes, a multiple of 4 (microscaled)
+    float *partial;          // splits > 1: [splits][x.rows][w.rows]
+};
+
+// BM rows of W times BN rows of X a block of WM x WN waves, NS stages of a step each in LDS: while one is multiplied, the
+// next NS - 1 are on their way.  Fragments m and m + 1 of a wave's rows of W interleave - the instruction's row 4 a + i is row
+// 8 a + 4 (m & 1) + i of the pair - so a lane ends with eight consecutive outputs of a token.
+template <int WK, int XK, int BM, int BN, int WM, int WN, int NS, class T>
+__global__ __launch_bounds__(WM *WN * 64) void k_product_tiled(operand w, operand x, tiling p, T *__restrict__ Y)
+{
+    constexpr int kWaves = WM * WN, kThreads = kWaves * 64, FM = BM / WM / 16, FN = BN / WN / 16;
+    constexpr int kWBytes = BM * step_of<WK>::bytes, kXBytes = BN * step_of<XK>::bytes;
+    constexpr int kScales = WK == kBF16 ? 0 : (BM + BN) * 4;
+    constexpr int kStage = kWBytes + kXBytes + kScales;
+    constexpr int kWLoads = kWBytes / 1024 / kWaves, kXLoads = kXBytes / 1024 / kWaves;
+    constexpr int kSLoads = WK == kBF16 ? 0 : (BM + BN) / 64 / kWaves;
+    constexpr int kLoads = kWLoads + kXLoads + kSLoads;
+    static_assert(kWLoads * 1024 * kWaves == kWBytes && kXLoads * 1024 * kWaves == kXBytes, "whole loads a wave");
+    static_assert(WK == kBF16 || (kSLoads * 64 * kWaves == BM + BN && BM % 64 == 0), "whole loads of scales a wave");
+    static_assert(FM % 2 == 0, "pairs of fragments");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[NS * kStage];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int q = lane >> 4, r = lane & 15;
+    // blocks are dealt to the eight dies in turn: each die gets a stretch of the tiles, and walks it in bands of four tiles
+    // of X, so that what its blocks read together stays in its L2
+    const int tiles = p.wtiles * p.xtiles, split = blockIdx.x / tiles;
+    int tile = blockIdx.x - split * tiles;
+    {
+        const int die = tile & 7, per = tiles >> 3, extra = tiles & 7;
+        tile = die * per + min(die, extra) + (tile >> 3);
+    }
+    const int band = tile / (4 * p.wtiles), in_band = tile - band * 4 * p.wtiles, deep = min(4, p.xtiles - band * 4);
+    const int wt = in_band / deep, xt = band * 4 + in_band - wt * deep;
+    const int o0 = wt * BM, t0 = xt * BN;
+
+    const int all = (p.nblk + step_of<WK>::blocks - 1) / step_of<WK>::blocks;
+    const int s0 = (int)((int64_t)all * split / p.splits), s1 = (int)((int64_t)all * (split + 1) / p.splits);
+    const bool tail = s1 == all && p.nblk % step_of<WK>::blocks != 0;      // the last step is part of one
+    const int whole = s1 - s0 - (tail ? 1 : 0);
+
+    const unsigned base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
+    // sources of this wave's loads of a step; rows past the end repeat the last one, their results are not stored
+    const uint8_t *src[kLoads];
+    unsigned dst[kLoads];
+#pragma unroll
+    for (int i = 0; i < kWLoads; ++i) {
+        const int at = (i * kWaves + wave) * 64 + lane, row = at / step_of<WK>::pieces, c = at % step_of<WK>::pieces;
+        src[i] = w.codes + (int64_t)min(o0 + row, w.rows - 1) * w.pitch + (int64_t)s0 * step_of<WK>::bytes + (c ^ key_of<WK>(row)) * 16;
+        dst[i] = (i * kWaves + wave) * 1024;
+    }
+#pragma unroll
+    for (int i = 0; i < kXLoads; ++i) {
+        const int at = (i * kWaves + wave) * 64 + lane, row = at / step_of<XK>::pieces, c = at % step_of<XK>::pieces;
+        src[kWLoads + i] = x.codes + (int64_t)min(t0 + row, x.rows - 1) * x.pitch + (int64_t)s0 * step_of<XK>::bytes + (c ^ key_of<XK>(row)) * 16;
+        dst[kWLoads + i] = kWBytes + (i * kWaves + wave) * 1024;
+    }
+#pragma unroll
+    for (int i = 0; i < kSLoads; ++i) {
+        const int first = (i * kWaves + wave) * 64, row = first + lane;
+        src[kWLoads + kXLoads + i] = (first < BM ? w.scales + min(o0 + row, w.rows - 1) * p.scale_pitch
+                                                 : x.scales + min(t0 + row - BM, x.rows - 1) * p.scale_pitch) + (int64_t)s0 * 4;
+        dst[kWLoads + kXLoads + i] = kWBytes + kXBytes + first * 4;
+    }
+    auto fetch_step = [&](int stage) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const unsigned to = base + stage * kStage + dst[i];
+            if (i < kWLoads + kXLoads) fetch<16>(src[i], to);
+            else fetch<4>(src[i], to);
+            src[i] += i < kWLoads ? step_of<WK>::bytes : i < kWLoads + kXLoads ? step_of<XK>::bytes : 4;
+        }
+    };
+
+    // this lane's part of a fragment: row and pieces
+    const int wr = (wave / WN) * (BM / WM) + 8 * (r >> 2) + (r & 3), xr = (wave % WN) * (BN / WN) + r;
+    const int wat = wr * step_of<WK>::bytes, xat = xr * step_of<XK>::bytes;
+    f4v acc[FM][FN];
+#pragma unroll
+    for (int m = 0; m < FM; ++m)
+#pragma unroll
+        for (int n = 0; n < FN; ++n) acc[m][n] = f4v{0.0f, 0.0f, 0.0f, 0.0f};
+
+    auto compute = [&](const uint8_t *stage) {
+        const uint8_t *wl = stage, *xl = stage + kWBytes;
+        const uint8_t *wsc = stage + kWBytes + kXBytes, *xsc = wsc + BM * 4;
+        if constexpr (WK == kBF16) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                b8v b[FN];
+#pragma unroll
+                for (int n = 0; n < FN; ++n)
+                    b[n] = *reinterpret_cast<const b8v *>(xl + xat + n * 16 * 128 + ((q + 4 * j) ^ key_of<XK>(r)) * 16);
+#pragma unroll
+                for (int m = 0; m < FM; ++m) {
+                    const int row = (m >> 1) * 32 + (m & 1) * 4;
+                    const b8v a = *reinterpret_cast<const b8v *>(wl + wat + row * 128 + ((q + 4 * j) ^ key_of<WK>(wr + row)) * 16);
+#pragma unroll
+                    for (int n = 0; n < FN; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[n], acc[m][n], 0, 0, 0);
+                }
+            }
+        } else {
+            part<XK> b[FN];
+#pragma unroll
+            for (int n = 0; n < FN; ++n) {
+#pragma unroll
+                for (int j = 0; j < part<XK>::chunks; ++j)
+                    b[n].c[j] = *reinterpret_cast<const pv_u4 *>(xl + xat + n * 16 * step_of<XK>::bytes + ((q + 4 * j) ^ key_of<XK>(r)) * 16);
+                b[n].scale = xsc[(xr + n * 16) * 4 + q];
+            }
+#pragma unroll
+            for (int m = 0; m < FM; ++m) {
+                const int row = (m >> 1) * 32 + (m & 1) * 4;
+                part<WK> a;
+                a.c[0] = *reinterpret_cast<const pv_u4 *>(wl + wat + row * step_of<WK>::bytes + (q ^ key_of<WK>(wr + row)) * 16);
+                a.scale = wsc[(wr + row) * 4 + q];
+#pragma unroll
+                for (int n = 0; n < FN; ++n) acc[m][n] = multiply<false>(a, b[n], acc[m][n]);
+            }
+        }
+    };
+
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s)
+        if (s < whole) fetch_step(s);
+    int stage = 0;
+    for (int s = 0; s < whole; ++s) {
+        if (s + NS - 2 < whole) wait_and_meet<(NS - 2) * kLoads>();
+        else wait_and_meet<0>();
+        if (s + NS - 1 < whole) fetch_step(stage == 0 ? NS - 1 : stage - 1);
+        compute(lds + stage * kStage);
+        stage = stage + 1 == NS ? 0 : stage + 1;
+    }
+    if (tail) {
+        // through registers, with zeros behind the row's last block; this stage's readers have met since
+        const int b0 = (s1 - 1) * step_of<WK>::blocks;
+        auto copy = [&](auto kind, const operand &o, int first, int rows, unsigned at) {
+            constexpr int KIND = decltype(kind)::value, kPieces = step_of<KIND>::pieces, kPerBlock = kPieces / step_of<KIND>::blocks;
+            for (int i = threadIdx.x; i < rows * kPieces; i += kThreads) {
+                const int row = i / kPieces, c = i % kPieces;
+                pv_u4 v = {0u, 0u, 0u, 0u};
+                if (b0 + c / kPerBlock < p.nblk)
+                    v = *reinterpret_cast<const pv_u4 *>(o.codes + (int64_t)min(first + row, o.rows - 1) * o.pitch + (int64_t)(s1 - 1) * step_of<KIND>::bytes + c * 16);
+                *reinterpret_cast<pv_u4 *>(lds + stage * kStage + at + row * step_of<KIND>::bytes + (c ^ key_of<KIND>(row)) * 16) = v;
+            }
+        };
+        copy(std::integral_constant<int, WK>{}, w, o0, BM, 0);
+        copy(std::integral_constant<int, XK>{}, x, t0, BN, kWBytes);
+        if constexpr (kScales != 0)
+            for (int row = threadIdx.x; row < BM + BN; row += kThreads) {
+                const uint8_t *from = row < BM ? w.scales + min(o0 + row, w.rows - 1) * p.scale_pitch
+                                               : x.scales + min(t0 + row - BM, x.rows - 1) * p.scale_pitch;
+                *reinterpret_cast<unsigned *>(lds + stage * kStage + kWBytes + kXBytes + row * 4) =
+                    *reinterpret_cast<const unsigned *>(from + (int64_t)(s1 - 1) * 4);
+            }
+        wait_and_meet<0>();
+        compute(lds + stage * kStage);
+    }
+#pragma unroll
+    for (int m = 0; m < FM; m += 2)
+#pragma unroll
+        for (int n = 0; n < FN; ++n) {
+            // every lane runs the last instructions, whatever it stores
+            asm volatile("" : "+v"(acc[m][n]), "+v"(acc[m + 1][n]));
+            const int o = o0 + (wave / WN) * (BM / WM) + m * 16 + q * 8, t = t0 + xr + n * 16;
+            if (t >= x.rows || o >= w.rows) continue;
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = acc[m][n][i], v[4 + i] = acc[m + 1][n][i];
+            if (p.splits == 1) pv_store8(Y + (int64_t)t * w.rows + o, w.rows - o, v);
+            else pv_store8(p.partial + ((int64_t)split * x.rows + t) * w.rows + o, w.rows - o, v);
+        }
+}
+
+// the splits' sums added in their order
+template <class T>
+__global__ __launch_bounds__(256) void k_add_splits(const float *__restrict__ partial, int splits, int64_t n, T *__restrict__ Y)
+{
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (at >= n) return;
+    const int valid = (int)min(n - at, (int64_t)8);
+    float v[8];
+    pv_load8(partial + at, valid, v);
+    for (int s = 1; s < splits; ++s) {
+        float u[8];
+        pv_load8(partial + s * n + at, valid, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += u[i];
+    }
+    pv_store8(Y + at, valid, v);
+}
+
+// scales with rows of a pitch that is a multiple of 4, zeros behind
+__global__ __launch_bounds__(256) void k_pad_scales(const uint8_t *__restrict__ in, int64_t rows, int nblk, uint8_t *__restrict__ out, int pitch)
+{
+    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, per = pitch / 4, row = u / per;
+    if (row >= rows) return;
+    const int c = (int)(u - row * per) * 4;
+    unsigned v = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v |= (c + i < nblk ? (unsigned)in[row * nblk + c + i] : 0u) << (8 * i);
+    reinterpret_cast<unsigned *>(out)[u] = v;
+}
+
 // ---------------------------------------------------------------- operands of the gradients
 
 // A matrix [rows, cols] (codes, or bf16) as bf16, transposed: out [cols, pitch] with pitch >= rows, zeros behind `rows`.
@@ -228,9 +471,28 @@ __global__ __launch_bounds__(256) void k_pad_rows(const pv_bf16 *__restrict__ in
     pv_store8(out + row * pitch + col, 8, v);
 }
 
+template <int WK, int XK, int BM, int BN, int WM, int WN, int NS, class T>
+pv_status launch_tiled(pv_ctx *ctx, const operand &w, const operand &x, tiling p, T *Y)
+{
+    p.wtiles = (w.rows + BM - 1) / BM;
+    p.xtiles = (x.rows + BN - 1) / BN;
+    const int64_t blocks = (int64_t)p.wtiles * p.xtiles * p.splits;
+    if (blocks >= (int64_t)1 << 31) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many tiles of the product");
+    hipLaunchKernelGGL((k_product_tiled<WK, XK, BM, BN, WM, WN, NS, T>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0, ctx->stream, w, x, p, Y);
+    PV_HIP(ctx, hipGetLastError());
+    return PV_OK;
+}
+
 template <int WK, int XK, class T, bool WIDE = std::is_same<T, float>::value && XK == kE4M3>
 pv_status launch(pv_ctx *ctx, const operand &w, const operand &x, int nblk, T *Y)
 {
+    if constexpr (!WIDE) {
+        tiling p = {nblk, 0, 0, 1, nblk, nullptr};
+        if (x.rows > 64 && (WK == kBF16 || nblk % 4 == 0)) {
+            constexpr int NS = WK == kBF16 ? 2 : 3;
+            return launch_tiled<WK, XK, 256, 256, 2, 4, NS>(ctx, w, x, p, Y);
+        }
+    }
     const int wtiles = (w.rows + 15) / 16;
     const int nt = x.rows <= 16 ? 1 : 4;
     const int64_t blocks = (int64_t)wtiles * ((x.rows + 16 * nt - 1) / (16 * nt));
