@@ -14,6 +14,7 @@ namespace {
 
 typedef int i8v __attribute__((ext_vector_type(8)));
 typedef float f4v __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
 typedef pv_bf16 b8v __attribute__((ext_vector_type(8)));
 typedef pv_bf16 b4v __attribute__((ext_vector_type(4)));
 
@@ -28,11 +29,10 @@ struct operand {
 
 // Bytes of 128 values of a row, and where a lane's part of them lies: lane group q = lane / 16 holds values
 // 32 q .. 32 q + 31 of E2M1, but 16 q .. + 15 and 64 + 16 q .. + 15 of E4M3; its scale is that of block q in either
-// case.  bf16: four instructions of 32 values, 8 q .. 8 q + 7 of each.
+// case.
 template <int KIND>
 struct part {
-    static constexpr int bytes = KIND == kE2M1 ? 64 : KIND == kE4M3 ? 128 : 256;
-    static constexpr int chunks = KIND == kE2M1 ? 1 : KIND == kE4M3 ? 2 : 4;      // of 16 bytes, 4 lane groups each
+    static constexpr int chunks = KIND == kE2M1 ? 1 : 2;      // of 16 bytes, 4 lane groups each
     pv_u4 c[chunks];
     unsigned scale;
 };
@@ -52,12 +52,12 @@ __device__ __forceinline__ void load_part(part<KIND> &p, const uint8_t *row, con
     for (int j = 0; j < part<KIND>::chunks; ++j) {
         // the chunk's place among the row's 16-byte pieces, and the block of 32 values that it belongs to
         const int piece = piece_of<KIND, WIDE>(step, j, q);
-        const int block = KIND == kE2M1 ? piece : KIND == kE4M3 ? piece >> 1 : piece >> 2;
+        const int block = KIND == kE2M1 ? piece : piece >> 1;
         p.c[j] = pv_u4{0u, 0u, 0u, 0u};
         if (block < nblk) p.c[j] = *reinterpret_cast<const pv_u4 *>(row + (int64_t)piece * 16);
     }
     p.scale = 127u;
-    if (KIND != kBF16 && step * 4 + q < nblk) p.scale = scale_row[step * 4 + q];
+    if (step * 4 + q < nblk) p.scale = scale_row[step * 4 + q];
 }
 
 // eight values, 8 j .. 8 j + 7 of the lane's block, as bf16
@@ -92,12 +92,6 @@ __device__ __forceinline__ f4v multiply(const part<WK> &w, const part<XK> &x, f4
         const float wp = pv_mx_power(w.scale), xp = pv_mx_power(x.scale);
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(w, j, wp), widen(x, j, xp), acc, 0, 0, 0);
-        return acc;
-    } else if constexpr (WK == kBF16) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8v, w.c[j]), __builtin_bit_cast(b8v, x.c[j]), acc,
-                                                         0, 0, 0);
         return acc;
     } else {
         i8v a = {0, 0, 0, 0, 0, 0, 0, 0}, b = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -178,16 +172,17 @@ __global__ __launch_bounds__(256) void k_product_direct(operand w, operand x, in
 
 // ---------------------------------------------------------------- tiles through LDS
 
-// A step is 128 values of a microscaled row or 64 of a bf16 one: `bytes` of it, in pieces of 16.
+// A step is 128 values of a microscaled row or 64 of a bf16 one: `bytes` of it, in pieces of 16.  It is multiplied in slices, one
+// instruction's depth each: 32 x 32 x 64 on codes, 32 x 32 x 16 on bf16.
 template <int KIND>
 struct step_of {
     static constexpr int bytes = KIND == kE2M1 ? 64 : 128, pieces = bytes / 16;
     static constexpr int values = KIND == kBF16 ? 64 : 128, blocks = values / 32;
+    static constexpr int slices = KIND == kBF16 ? 4 : 2;
 };
 
 // Where piece c of a tile's row lies in LDS: rows are `bytes` apart, and the pieces of a row change places by a key
-// of the row, so that the eight lanes that read at a time - rows 8 a + 0 .. 3 and 8 a + 8 .. 11 of a pair of fragments, the same
-// piece - meet 32 different banks.
+// of the row, so that lanes which read the same piece of neighbouring rows meet different banks.
 template <int KIND>
 __device__ __forceinline__ int key_of(int row)
 {
@@ -195,16 +190,46 @@ __device__ __forceinline__ int key_of(int row)
     return (row >> 1 & 1) | (row >> 3 & 1) << 1;
 }
 
-// BYTES (16 or 4) a lane from memory to LDS, lane i to `to` + BYTES * i
+// A lane's part of 32 rows of a slice: 32 values of codes (lane group h = lane / 32: block h; E4M3 in two halves of 16 values, 16 h
+// and 32 + 16 h), or 8 values of bf16, 8 h.
+template <int KIND>
+struct frag {
+    pv_u4 c[KIND == kE4M3 ? 2 : 1];
+};
+
+template <int KIND>
+__device__ __forceinline__ int piece_in_step(int slice, int c, int h)
+{
+    return KIND == kE4M3 ? slice * 4 + c * 2 + h : slice * 2 + h;
+}
+
+// ws, xs: the scales of the step's blocks h and 2 + h in bytes 0 and 2; SEL: the slice's byte
+template <int SEL, int WK, int XK>
+__device__ __forceinline__ f16v multiply(const frag<WK> &w, unsigned ws, const frag<XK> &x, unsigned xs, f16v acc)
+{
+    if constexpr (WK == kBF16) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8v, w.c[0]), __builtin_bit_cast(b8v, x.c[0]), acc, 0, 0, 0);
+    } else {
+        i8v a = {0, 0, 0, 0, 0, 0, 0, 0}, b = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = (int)w.c[0][i];
+#pragma unroll
+        for (int i = 0; i < (XK == kE4M3 ? 8 : 4); ++i) b[i] = (int)x.c[i / 4][i % 4];
+        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 4, XK == kE2M1 ? 4 : 0, SEL, (int)ws, SEL, (int)xs);
+    }
+}
+
+// BYTES (16 or 4) a lane from memory to LDS, lane i to `to` + BYTES * i.  An instruction and no builtin: behind the builtin the
+// compiler takes every later read of LDS for one that may be answered out of order, and waits for all of them at each use
+// (4096 x 8192 x 4096: 113 -> 107 us).  It has no result; the kernel waits for it by count.
 template <int BYTES>
 __device__ __forceinline__ void fetch(const void *from, unsigned to)
 {
-    const auto at = (__attribute__((address_space(3))) void *)(uintptr_t)to;
-    if constexpr (BYTES == 16) __builtin_amdgcn_global_load_lds(from, at, 16, 0, 0);
-    else __builtin_amdgcn_global_load_lds(from, at, 4, 0, 0);
+    if constexpr (BYTES == 16) asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(to) : "memory");
+    else asm volatile("global_load_lds_dword %0, off" ::"v"(from), "{m0}"(to) : "memory");
 }
 
-// All but the last N memory operations of this wave are done, and every wave has come here.
+// All but the last N memory operations of this wave are done, its reads of LDS too, and every wave has come here.
 template <int N>
 __device__ __forceinline__ void wait_and_meet()
 {
@@ -219,26 +244,30 @@ struct tiling {
     float *partial;          // splits > 1: [splits][x.rows][w.rows]
 };
 
-// BM rows of W times BN rows of X a block of WM x WN waves, NS stages of a step each in LDS: while one is multiplied, the
-// next NS - 1 are on their way.  Fragments m and m + 1 of a wave's rows of W interleave - the instruction's row 4 a + i is row
-// 8 a + 4 (m & 1) + i of the pair - so a lane ends with eight consecutive outputs of a token.
+// BM rows of W times BN rows of X a block of WM x WN waves, NS stages of a step each in LDS.
+// The matrix cores wait for nothing that can be asked for earlier: while a slice is multiplied, the next one is read from LDS into
+// a second set of registers, the first of the next step behind the last of this one.  So the waves meet before a step's last
+// slice: then all have this step in registers, its stage is free for the loads of step s + NS, and step s + 1 has arrived.
+// Rows of W are dealt to the instruction's rows so that a lane ends with eight consecutive outputs of a token: its row
+// 16 a + 8 b + 4 c + i (b, c bits, i < 4) is row 16 a + 8 c + 4 b + i.
 template <int WK, int XK, int BM, int BN, int WM, int WN, int NS, class T>
 __global__ __launch_bounds__(WM *WN * 64) void k_product_tiled(operand w, operand x, tiling p, T *__restrict__ Y)
 {
-    constexpr int kWaves = WM * WN, kThreads = kWaves * 64, FM = BM / WM / 16, FN = BN / WN / 16;
+    constexpr int kWaves = WM * WN, kThreads = kWaves * 64, FM = BM / WM / 32, FN = BN / WN / 32;
     constexpr int kWBytes = BM * step_of<WK>::bytes, kXBytes = BN * step_of<XK>::bytes;
-    constexpr int kScales = WK == kBF16 ? 0 : (BM + BN) * 4;
-    constexpr int kStage = kWBytes + kXBytes + kScales;
-    constexpr int kWLoads = kWBytes / 1024 / kWaves, kXLoads = kXBytes / 1024 / kWaves;
+    // scales: four steps of them at a time, 16 bytes a row, in two buffers behind the stages
+    constexpr int kScales = WK == kBF16 ? 0 : (BM + BN) * 16;
+    constexpr int kStage = kWBytes + kXBytes;
+    constexpr int kWLoads = kWBytes / 1024 / kWaves, kXLoads = kXBytes / 1024 / kWaves, kData = kWLoads + kXLoads;
     constexpr int kSLoads = WK == kBF16 ? 0 : (BM + BN) / 64 / kWaves;
-    constexpr int kLoads = kWLoads + kXLoads + kSLoads;
+    constexpr int kSlices = step_of<WK>::slices;
     static_assert(kWLoads * 1024 * kWaves == kWBytes && kXLoads * 1024 * kWaves == kXBytes, "whole loads a wave");
-    static_assert(WK == kBF16 || (kSLoads * 64 * kWaves == BM + BN && BM % 64 == 0), "whole loads of scales a wave");
-    static_assert(FM % 2 == 0, "pairs of fragments");
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[NS * kStage];
+    static_assert(WK == kBF16 || kSLoads * 64 * kWaves == BM + BN, "whole loads of scales a wave");
+    static_assert(BM % 16 == 0 && FM * 32 * WM == BM && FN * 32 * WN == BN && kSlices % 2 == 0 && NS >= 2, "tile");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[NS * kStage + 2 * kScales];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int q = lane >> 4, r = lane & 15;
+    const int h = lane >> 5, r = lane & 31;
     // blocks are dealt to the eight dies in turn: each die gets a stretch of the tiles, and walks it in bands of four tiles
     // of X, so that what its blocks read together stays in its L2
     const int tiles = p.wtiles * p.xtiles, split = blockIdx.x / tiles;
@@ -254,102 +283,56 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tiled(operand w, operan
     const int all = (p.nblk + step_of<WK>::blocks - 1) / step_of<WK>::blocks;
     const int s0 = (int)((int64_t)all * split / p.splits), s1 = (int)((int64_t)all * (split + 1) / p.splits);
     const bool tail = s1 == all && p.nblk % step_of<WK>::blocks != 0;      // the last step is part of one
-    const int whole = s1 - s0 - (tail ? 1 : 0);
+    const int steps = s1 - s0, whole = steps - (tail ? 1 : 0);
 
     const unsigned base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
-    // sources of this wave's loads of a step; rows past the end repeat the last one, their results are not stored
-    const uint8_t *src[kLoads];
-    unsigned dst[kLoads];
+    // Sources of this wave's loads of a step: a scalar address that moves with the steps, and a lane's 32-bit distance from it.
+    // Rows past the end repeat the last one, their results are not stored.
+    const uint8_t *wsrc = w.codes + (int64_t)o0 * w.pitch + (int64_t)s0 * step_of<WK>::bytes;
+    const uint8_t *xsrc = x.codes + (int64_t)t0 * x.pitch + (int64_t)s0 * step_of<XK>::bytes;
+    unsigned far[kData];
 #pragma unroll
     for (int i = 0; i < kWLoads; ++i) {
         const int at = (i * kWaves + wave) * 64 + lane, row = at / step_of<WK>::pieces, c = at % step_of<WK>::pieces;
-        src[i] = w.codes + (int64_t)min(o0 + row, w.rows - 1) * w.pitch + (int64_t)s0 * step_of<WK>::bytes + (c ^ key_of<WK>(row)) * 16;
-        dst[i] = (i * kWaves + wave) * 1024;
+        far[i] = (unsigned)min(row, w.rows - 1 - o0) * (unsigned)w.pitch + (c ^ key_of<WK>(row)) * 16;
     }
 #pragma unroll
     for (int i = 0; i < kXLoads; ++i) {
         const int at = (i * kWaves + wave) * 64 + lane, row = at / step_of<XK>::pieces, c = at % step_of<XK>::pieces;
-        src[kWLoads + i] = x.codes + (int64_t)min(t0 + row, x.rows - 1) * x.pitch + (int64_t)s0 * step_of<XK>::bytes + (c ^ key_of<XK>(row)) * 16;
-        dst[kWLoads + i] = kWBytes + (i * kWaves + wave) * 1024;
+        far[kWLoads + i] = (unsigned)min(row, x.rows - 1 - t0) * (unsigned)x.pitch + (c ^ key_of<XK>(row)) * 16;
     }
+    // loads `first` .. `last` - 1 of the next step that has not been asked for, into `stage`
+    auto fetch_some = [&](int stage, int first, int last) {
+        const unsigned to = base + stage * kStage + wave * 1024;
 #pragma unroll
-    for (int i = 0; i < kSLoads; ++i) {
-        const int first = (i * kWaves + wave) * 64, row = first + lane;
-        src[kWLoads + kXLoads + i] = (first < BM ? w.scales + min(o0 + row, w.rows - 1) * p.scale_pitch
-                                                 : x.scales + min(t0 + row - BM, x.rows - 1) * p.scale_pitch) + (int64_t)s0 * 4;
-        dst[kWLoads + kXLoads + i] = kWBytes + kXBytes + first * 4;
-    }
-    auto fetch_step = [&](int stage) {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const unsigned to = base + stage * kStage + dst[i];
-            if (i < kWLoads + kXLoads) fetch<16>(src[i], to);
-            else fetch<4>(src[i], to);
-            src[i] += i < kWLoads ? step_of<WK>::bytes : i < kWLoads + kXLoads ? step_of<XK>::bytes : 4;
+        for (int i = 0; i < kData; ++i) {
+            if (i < first || i >= last) continue;
+            if (i < kWLoads) fetch<16>(wsrc + far[i], to + i * kWaves * 1024);
+            else fetch<16>(xsrc + far[i], to + kWBytes + (i - kWLoads) * kWaves * 1024);
+        }
+        if (last == kData) {
+            wsrc += step_of<WK>::bytes;
+            xsrc += step_of<XK>::bytes;
         }
     };
-
-    // this lane's part of a fragment: row and pieces
-    const int wr = (wave / WN) * (BM / WM) + 8 * (r >> 2) + (r & 3), xr = (wave % WN) * (BN / WN) + r;
-    const int wat = wr * step_of<WK>::bytes, xat = xr * step_of<XK>::bytes;
-    f4v acc[FM][FN];
+    auto fetch_step = [&](int stage) { fetch_some(stage, 0, kData); };
+    // A load of scales: 16 rows, four steps of one row side by side, so that a line of memory is asked for once in four steps.
+    // What lies behind the row's end is not used and stands for the last blocks.
+    const int wlast = w.rows - 1 - o0, xlast = x.rows - 1 - t0, last_scales = ((p.nblk - 1) & ~3) - s0 * 4;
+    const uint8_t *wscale = w.scales + (int64_t)o0 * p.scale_pitch + (int64_t)s0 * 4, *xscale = x.scales + (int64_t)t0 * p.scale_pitch + (int64_t)s0 * 4;
+    auto fetch_scales = [&](int quarter, int group) {
+        if (WK == kBF16) return;
+        const unsigned at = (unsigned)min((group * 4 + (lane & 3)) * 4, last_scales);
 #pragma unroll
-    for (int m = 0; m < FM; ++m)
-#pragma unroll
-        for (int n = 0; n < FN; ++n) acc[m][n] = f4v{0.0f, 0.0f, 0.0f, 0.0f};
-
-    auto compute = [&](const uint8_t *stage) {
-        const uint8_t *wl = stage, *xl = stage + kWBytes;
-        const uint8_t *wsc = stage + kWBytes + kXBytes, *xsc = wsc + BM * 4;
-        if constexpr (WK == kBF16) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                b8v b[FN];
-#pragma unroll
-                for (int n = 0; n < FN; ++n)
-                    b[n] = *reinterpret_cast<const b8v *>(xl + xat + n * 16 * 128 + ((q + 4 * j) ^ key_of<XK>(r)) * 16);
-#pragma unroll
-                for (int m = 0; m < FM; ++m) {
-                    const int row = (m >> 1) * 32 + (m & 1) * 4;
-                    const b8v a = *reinterpret_cast<const b8v *>(wl + wat + row * 128 + ((q + 4 * j) ^ key_of<WK>(wr + row)) * 16);
-#pragma unroll
-                    for (int n = 0; n < FN; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[n], acc[m][n], 0, 0, 0);
-                }
-            }
-        } else {
-            part<XK> b[FN];
-#pragma unroll
-            for (int n = 0; n < FN; ++n) {
-#pragma unroll
-                for (int j = 0; j < part<XK>::chunks; ++j)
-                    b[n].c[j] = *reinterpret_cast<const pv_u4 *>(xl + xat + n * 16 * step_of<XK>::bytes + ((q + 4 * j) ^ key_of<XK>(r)) * 16);
-                b[n].scale = xsc[(xr + n * 16) * 4 + q];
-            }
-#pragma unroll
-            for (int m = 0; m < FM; ++m) {
-                const int row = (m >> 1) * 32 + (m & 1) * 4;
-                part<WK> a;
-                a.c[0] = *reinterpret_cast<const pv_u4 *>(wl + wat + row * step_of<WK>::bytes + (q ^ key_of<WK>(wr + row)) * 16);
-                a.scale = wsc[(wr + row) * 4 + q];
-#pragma unroll
-                for (int n = 0; n < FN; ++n) acc[m][n] = multiply<false>(a, b[n], acc[m][n]);
-            }
+        for (int i = 0; i < kSLoads; ++i) {
+            const int first = ((quarter * kSLoads + i) * kWaves + wave) * 16;
+            const bool of_w = first < BM;
+            const int row = min((of_w ? first : first - BM) + (lane >> 2), of_w ? wlast : xlast);
+            fetch<4>((of_w ? wscale : xscale) + ((unsigned)row * (unsigned)p.scale_pitch + at), base + NS * kStage + (group & 1) * kScales + first * 16);
         }
     };
-
-#pragma unroll
-    for (int s = 0; s < NS - 1; ++s)
-        if (s < whole) fetch_step(s);
-    int stage = 0;
-    for (int s = 0; s < whole; ++s) {
-        if (s + NS - 2 < whole) wait_and_meet<(NS - 2) * kLoads>();
-        else wait_and_meet<0>();
-        if (s + NS - 1 < whole) fetch_step(stage == 0 ? NS - 1 : stage - 1);
-        compute(lds + stage * kStage);
-        stage = stage + 1 == NS ? 0 : stage + 1;
-    }
-    if (tail) {
-        // through registers, with zeros behind the row's last block; this stage's readers have met since
+    // The step that is part of one: through registers, with zeros behind the row's last block.
+    auto copy_tail = [&](int stage) {
         const int b0 = (s1 - 1) * step_of<WK>::blocks;
         auto copy = [&](auto kind, const operand &o, int first, int rows, unsigned at) {
             constexpr int KIND = decltype(kind)::value, kPieces = step_of<KIND>::pieces, kPerBlock = kPieces / step_of<KIND>::blocks;
@@ -363,29 +346,118 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tiled(operand w, operan
         };
         copy(std::integral_constant<int, WK>{}, w, o0, BM, 0);
         copy(std::integral_constant<int, XK>{}, x, t0, BN, kWBytes);
-        if constexpr (kScales != 0)
-            for (int row = threadIdx.x; row < BM + BN; row += kThreads) {
-                const uint8_t *from = row < BM ? w.scales + min(o0 + row, w.rows - 1) * p.scale_pitch
-                                               : x.scales + min(t0 + row - BM, x.rows - 1) * p.scale_pitch;
-                *reinterpret_cast<unsigned *>(lds + stage * kStage + kWBytes + kXBytes + row * 4) =
-                    *reinterpret_cast<const unsigned *>(from + (int64_t)(s1 - 1) * 4);
-            }
-        wait_and_meet<0>();
-        compute(lds + stage * kStage);
-    }
+    };
+
+    // this lane's rows of the first fragments
+    const int wr = (wave / WN) * (BM / WM) + ((r & 19) | (r >> 2 & 1) << 3 | (r >> 3 & 1) << 2), xr = (wave % WN) * (BN / WN) + r;
+    frag<WK> a[FM];
+    frag<XK> b[2][FN];
+    unsigned ws[FM], xs[FN], xs_next[FN];      // scales as they come, four blocks a row; of the step at hand moved to this lane's blocks
+    auto read_x = [&](int set, int stage, int step, int slice) {
+        const uint8_t *xl = lds + stage * kStage + kWBytes + xr * step_of<XK>::bytes;
+        const uint8_t *sc = lds + NS * kStage + (step >> 2 & 1) * kScales + (step & 3) * 4;
 #pragma unroll
-    for (int m = 0; m < FM; m += 2)
+        for (int n = 0; n < FN; ++n) {
+#pragma unroll
+            for (int c = 0; c < (XK == kE4M3 ? 2 : 1); ++c)
+                b[set][n].c[c] = *reinterpret_cast<const pv_u4 *>(xl + n * 32 * step_of<XK>::bytes + (piece_in_step<XK>(slice, c, h) ^ key_of<XK>(xr)) * 16);
+            if (WK != kBF16 && slice == 0) xs_next[n] = *reinterpret_cast<const unsigned *>(sc + (BM + xr + n * 32) * 16);
+        }
+    };
+    auto read_w = [&](int m, int stage, int step, int slice) {
+        const uint8_t *wl = lds + stage * kStage + wr * step_of<WK>::bytes;
+        const uint8_t *sc = lds + NS * kStage + (step >> 2 & 1) * kScales + (step & 3) * 4;
+        a[m].c[0] = *reinterpret_cast<const pv_u4 *>(wl + m * 32 * step_of<WK>::bytes + (piece_in_step<WK>(slice, 0, h) ^ key_of<WK>(wr)) * 16);
+        if (WK != kBF16 && slice == 0) ws[m] = *reinterpret_cast<const unsigned *>(sc + (wr + m * 32) * 16);
+    };
+    f16v acc[FM][FN];
+#pragma unroll
+    for (int m = 0; m < FM; ++m)
+#pragma unroll
+        for (int n = 0; n < FN; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[m][n][i] = 0.0f;
+
+#pragma unroll
+    for (int i = 0; i < 4; ++i) fetch_scales(i, 0);
+    if (steps > 4) fetch_scales(0, 1);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        if (s < whole) fetch_step(s);
+        else if (s == whole && tail) copy_tail(s);
+    }
+    if (NS <= whole) wait_and_meet<(NS - 1) * kData>();
+    else wait_and_meet<0>();
+    read_x(0, 0, 0, 0);
+#pragma unroll
+    for (int m = 0; m < FM; ++m) read_w(m, 0, 0, 0);
+    // Loads that may be on their way when step s + 1 has to have arrived: those of the steps s + 2 .. s + NS - 1; of scales, the last
+    // ones that are needed were asked for right before the last of those steps.
+    constexpr int kAhead = (WK == kBF16 ? NS - 2 : NS > 2 ? 1 : 0) * kData;
+    int stage = 0;
+    // A step.  FULL: there is a whole step s + NS, and no condition stands between the instructions.  What is read behind the last
+    // step is not used.
+    auto step = [&](auto full, int s) {
+        constexpr bool FULL = decltype(full)::value;
+        const int after = stage + 1 == NS ? 0 : stage + 1;
+#pragma unroll
+        for (int j = 0; j < kSlices; ++j) {
+            const bool last = j + 1 == kSlices;
+            const int to_stage = last ? after : stage, to_step = last ? s + 1 : s, to_slice = last ? 0 : j + 1;
+            if (!last) read_x((j + 1) & 1, to_stage, to_step, to_slice);
+            // a fragment of W's rows is read over as soon as its instructions have taken it
+#pragma unroll
+            for (int m = 0; m < FM; ++m) {
+                __builtin_amdgcn_sched_barrier(0);
+                if (j == 0 && WK != kBF16) {
+                    ws[m] >>= 8 * h;
+#pragma unroll
+                    for (int n = 0; n < FN; ++n)
+                        if (m == 0) xs[n] = xs_next[n] >> (8 * h);
+                }
+#pragma unroll
+                for (int n = 0; n < FN; ++n)
+                    acc[m][n] = j & 1 ? multiply<2>(a[m], ws[m], b[j & 1][n], xs[n], acc[m][n]) : multiply<0>(a[m], ws[m], b[j & 1][n], xs[n], acc[m][n]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (last && m == 0) {
+                    if constexpr (FULL) {
+                        wait_and_meet<kAhead>();
+                        fetch_scales((s + 1) & 3, ((s + 1) >> 2) + 1);
+                    } else {
+                        wait_and_meet<0>();
+                        if ((((s + 1) >> 2) + 1) * 4 < steps) fetch_scales((s + 1) & 3, ((s + 1) >> 2) + 1);
+                        if (s + NS == whole && tail) copy_tail(stage);
+                    }
+                    read_x(0, to_stage, to_step, to_slice);
+                }
+                if (FULL && last) fetch_some(stage, m * kData / FM, (m + 1) * kData / FM);
+                read_w(m, to_stage, to_step, to_slice);
+            }
+        }
+        stage = after;
+    };
+    __builtin_amdgcn_s_waitcnt(0xC07F);        // lgkmcnt(0), seen by the compiler: no scalar load is left that its count would have to allow for
+    int s = 0;
+    for (; s + NS < whole; ++s) step(std::true_type{}, s);
+    for (; s < steps; ++s) step(std::false_type{}, s);
+#pragma unroll
+    for (int m = 0; m < FM; ++m)
 #pragma unroll
         for (int n = 0; n < FN; ++n) {
             // every lane runs the last instructions, whatever it stores
-            asm volatile("" : "+v"(acc[m][n]), "+v"(acc[m + 1][n]));
-            const int o = o0 + (wave / WN) * (BM / WM) + m * 16 + q * 8, t = t0 + xr + n * 16;
-            if (t >= x.rows || o >= w.rows) continue;
-            float v[8];
+            asm volatile("" : "+v"(acc[m][n]));
+            const int t = t0 + xr + n * 32;
+            if (t >= x.rows) continue;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = acc[m][n][i], v[4 + i] = acc[m + 1][n][i];
-            if (p.splits == 1) pv_store8(Y + (int64_t)t * w.rows + o, w.rows - o, v);
-            else pv_store8(p.partial + ((int64_t)split * x.rows + t) * w.rows + o, w.rows - o, v);
+            for (int e = 0; e < 2; ++e) {
+                const int o = o0 + (wave / WN) * (BM / WM) + m * 32 + e * 16 + h * 8;
+                if (o >= w.rows) continue;
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = acc[m][n][e * 8 + i];
+                if (p.splits == 1) pv_store8(Y + (int64_t)t * w.rows + o, w.rows - o, v);
+                else pv_store8(p.partial + ((int64_t)split * x.rows + t) * w.rows + o, w.rows - o, v);
+            }
         }
 }
 
@@ -471,38 +543,83 @@ __global__ __launch_bounds__(256) void k_pad_rows(const pv_bf16 *__restrict__ in
     pv_store8(out + row * pitch + col, 8, v);
 }
 
+// ---------------------------------------------------------------- which kernel
+
+constexpr int kDirect = 0, kSmallTile = 1, kLargeTile = 2;
+
+struct choice {
+    int tile, splits;
+    size_t partial;          // bytes of the splits' sums
+};
+
+// The variant that is expected to take least, from what the parts take (us): a step of a large tile on each of 256 compute units, of
+// two small tiles on each, or of one; a launch's start and end; another launch that adds the splits' sums, which are
+// written and read.  Measured on 4096 in -> 4096 out, e4m3, bf16 out (small tiles with 1, 2, 4, 8 splits | large ones with 1, 2, 4):
+//   128 tokens 18.0 16.2 15.8 19.6 | 41.6 29.4 23.6      512 tokens 19.5 21.6 25.8 35.3 | 43.8 37.0 30.9
+//   2048 tokens 37.2 60.5 81.2 133 | 47.9 52.0 72.3      131 tokens of 14336, both e2m1: 40.5 27.2 20.8 24.3 | 90.4 53.7 35.1
+// Up to 16 tokens W is read straight to registers, at any size: 16 rows of X fill one instruction (32 tokens, 4096 -> 11008:
+// 28.5 us that way, 14.7 through tiles).
+template <int WK, int XK>
+choice choose(int64_t out, int64_t tokens, int nblk)
+{
+    constexpr double kStep = WK == kBF16 ? 1.5 : XK == kE4M3 ? 1.6 : 1.15;
+    constexpr double kTwoSmall = 0.6 * kStep, kOneSmall = (WK == kBF16 ? 0.4 : 0.3) * kStep;
+    const int steps = (nblk + step_of<WK>::blocks - 1) / step_of<WK>::blocks;
+    choice best = {kLargeTile, 1, 0};
+    double least = 1e300;
+    for (int tile = kSmallTile; tile <= kLargeTile; ++tile) {
+        const int side = tile == kLargeTile ? 256 : 128, at_once = tile == kLargeTile ? 256 : 512;
+        const int64_t tiles = ((out + side - 1) / side) * ((tokens + side - 1) / side);
+        for (int splits = 1; splits <= 16 && splits * 4 <= (steps > 4 ? steps : 4); splits *= 2) {
+            const int64_t blocks = tiles * splits, rounds = blocks / at_once, rest = blocks % at_once;
+            const double mine = (steps + splits - 1) / splits, full = tile == kLargeTile ? kStep : kTwoSmall;
+            double us = (double)rounds * (mine * full + 4.0);
+            if (rest) us += mine * (tile == kSmallTile && rest <= 256 ? kOneSmall : full) + 4.0;
+            if (splits > 1) us += 4.0 + (double)splits * (double)(out * tokens) * 8 / 4e6;
+            if (us < least) least = us, best = {tile, splits, splits > 1 ? (size_t)(splits * out * tokens) * 4 : 0};
+        }
+    }
+    return best;
+}
+
 template <int WK, int XK, int BM, int BN, int WM, int WN, int NS, class T>
 pv_status launch_tiled(pv_ctx *ctx, const operand &w, const operand &x, tiling p, T *Y)
 {
+    // a tile's rows lie within 32 bits of its first
+    if (w.pitch >= 1 << 24 || x.pitch >= 1 << 24) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "more than 16 MiB a row of an operand");
     p.wtiles = (w.rows + BM - 1) / BM;
     p.xtiles = (x.rows + BN - 1) / BN;
     const int64_t blocks = (int64_t)p.wtiles * p.xtiles * p.splits;
     if (blocks >= (int64_t)1 << 31) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many tiles of the product");
     hipLaunchKernelGGL((k_product_tiled<WK, XK, BM, BN, WM, WN, NS, T>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0, ctx->stream, w, x, p, Y);
     PV_HIP(ctx, hipGetLastError());
+    if (p.splits == 1) return PV_OK;
+    const int64_t n = (int64_t)x.rows * w.rows, sums = (n + 2047) / 2048;
+    if (sums >= (int64_t)1 << 31) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many outputs of the product");
+    hipLaunchKernelGGL((k_add_splits<T>), dim3((unsigned)sums), dim3(256), 0, ctx->stream, p.partial, p.splits, n, Y);
+    PV_HIP(ctx, hipGetLastError());
     return PV_OK;
 }
 
-template <int WK, int XK, class T, bool WIDE = std::is_same<T, float>::value && XK == kE4M3>
-pv_status launch(pv_ctx *ctx, const operand &w, const operand &x, int nblk, T *Y)
+template <bool WIDE, int WK, int XK, int NT, class T>
+pv_status launch_direct(pv_ctx *ctx, const operand &w, const operand &x, int nblk, T *Y)
 {
-    if constexpr (!WIDE) {
-        tiling p = {nblk, 0, 0, 1, nblk, nullptr};
-        if (x.rows > 64 && (WK == kBF16 || nblk % 4 == 0)) {
-            constexpr int NS = WK == kBF16 ? 2 : 3;
-            return launch_tiled<WK, XK, 256, 256, 2, 4, NS>(ctx, w, x, p, Y);
-        }
-    }
     const int wtiles = (w.rows + 15) / 16;
-    const int nt = x.rows <= 16 ? 1 : 4;
-    const int64_t blocks = (int64_t)wtiles * ((x.rows + 16 * nt - 1) / (16 * nt));
+    const int64_t blocks = (int64_t)wtiles * ((x.rows + 16 * NT - 1) / (16 * NT));
     if (blocks >= (int64_t)1 << 31) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many tiles of the product");
-    if (nt == 1)
-        hipLaunchKernelGGL((k_product_direct<WIDE, WK, XK, 1, T>), dim3((unsigned)blocks), dim3(256), 0, ctx->stream, w, x, nblk, Y, wtiles);
-    else
-        hipLaunchKernelGGL((k_product_direct<WIDE, WK, XK, 4, T>), dim3((unsigned)blocks), dim3(256), 0, ctx->stream, w, x, nblk, Y, wtiles);
+    hipLaunchKernelGGL((k_product_direct<WIDE, WK, XK, NT, T>), dim3((unsigned)blocks), dim3(256), 0, ctx->stream, w, x, nblk, Y, wtiles);
     PV_HIP(ctx, hipGetLastError());
     return PV_OK;
+}
+
+// w, x: with scale rows of `scale_pitch` bytes, a multiple of 4; partial: room for the splits' sums
+template <int WK, int XK, class T>
+pv_status launch(pv_ctx *ctx, const choice &c, const operand &w, const operand &x, int nblk, int64_t scale_pitch, float *partial, T *Y)
+{
+    const tiling p = {nblk, 0, 0, c.splits, scale_pitch, partial};
+    constexpr int NS = WK == kBF16 ? 2 : 3;
+    if (c.tile == kSmallTile) return launch_tiled<WK, XK, 128, 128, 2, 2, NS>(ctx, w, x, p, Y);
+    return launch_tiled<WK, XK, 256, 256, 2, 4, NS>(ctx, w, x, p, Y);
 }
 
 operand coded(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, int format)
@@ -513,6 +630,9 @@ operand coded(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t
 operand plain(const void *p, int64_t rows, int64_t pitch) { return {static_cast<const uint8_t *>(p), nullptr, pitch * 2, (int)rows}; }
 
 int64_t padded(int64_t n) { return pv_mx_blocks(n) * kMxBlock; }
+
+
+size_t round16(size_t bytes) { return (bytes + 15) & ~(size_t)15; }
 
 pv_status transpose(pv_ctx *ctx, int kind, const void *codes, const uint8_t *scales, int64_t rows, int64_t cols, pv_bf16 *out)
 {
@@ -525,19 +645,72 @@ pv_status transpose(pv_ctx *ctx, int kind, const void *codes, const uint8_t *sca
     return PV_OK;
 }
 
+// a matrix of codes as bf16 rows of whole blocks
+pv_status widen(pv_ctx *ctx, int format, const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *out)
+{
+    return pv_launch_dequantize_mx(ctx, rows, padded(cols), format, codes, scales, PV_BF16, out);
+}
+
 }  // namespace
 
 pv_status pv_launch_mx_product(pv_ctx *ctx, int64_t tokens, int64_t out, int64_t in, int x_format,
                                const uint8_t *x_codes, const uint8_t *x_scales, const uint8_t *w_codes,
                                const uint8_t *w_scales, int y_type, void *Y)
 {
-    pv_timed t(ctx, PV_K_MX_PRODUCT);
-    const operand w = coded(w_codes, w_scales, out, in, PV_MX_E2M1), x = coded(x_codes, x_scales, tokens, in, x_format);
+    operand w = coded(w_codes, w_scales, out, in, PV_MX_E2M1), x = coded(x_codes, x_scales, tokens, in, x_format);
     const int nblk = (int)pv_mx_blocks(in);
+    const bool wide = y_type == PV_F32 && x_format == PV_MX_E4M3;
+    const choice c = tokens <= 16 ? choice{kDirect, 1, 0}
+                   : wide ? choose<kBF16, kBF16>(out, tokens, nblk)
+                   : x_format == PV_MX_E2M1 ? choose<kE2M1, kE2M1>(out, tokens, nblk) : choose<kE2M1, kE4M3>(out, tokens, nblk);
+    if (c.tile == kDirect) {
+        pv_timed t(ctx, PV_K_MX_PRODUCT);
+        return pv_for_dtype(y_type, [&](auto v) {
+            using T = decltype(v);
+            T *y = static_cast<T *>(Y);
+            if (x_format == PV_MX_E2M1) return launch_direct<false, kE2M1, kE2M1, 1>(ctx, w, x, nblk, y);
+            return launch_direct<std::is_same<T, float>::value, kE2M1, kE4M3, 1>(ctx, w, x, nblk, y);
+        });
+    }
+    // scratch: both sides as bf16, or scales with rows of whole words; the splits' sums
+    const int64_t pitch = (nblk + 3) & ~3, k = padded(in);
+    const bool pad = !wide && pitch != nblk;
+    const size_t wb = round16(wide ? (size_t)(out * k) * 2 : pad ? (size_t)(out * pitch) : 0);
+    const size_t xb = round16(wide ? (size_t)(tokens * k) * 2 : pad ? (size_t)(tokens * pitch) : 0);
+    void *scratch = nullptr;
+    if (wb + xb + c.partial) {
+        const pv_status st = pv_ops_scratch(ctx, wb + xb + c.partial, &scratch);
+        if (st != PV_OK) return st;
+    }
+    uint8_t *ws = static_cast<uint8_t *>(scratch), *xs = ws + wb;
+    float *partial = reinterpret_cast<float *>(xs + xb);
+    pv_timed t(ctx, PV_K_MX_PRODUCT);
+    if (wide) {
+        pv_status st = widen(ctx, PV_MX_E2M1, w_codes, w_scales, out, in, ws);
+        if (st == PV_OK) st = widen(ctx, PV_MX_E4M3, x_codes, x_scales, tokens, in, xs);
+        if (st != PV_OK) return st;
+        return launch<kBF16, kBF16>(ctx, c, plain(ws, out, k), plain(xs, tokens, k), nblk, 0, partial, static_cast<float *>(Y));
+    }
+    if (pad) {
+        auto words = [&](const uint8_t *from, int64_t rows, uint8_t *to) {
+            const int64_t blocks = (rows * (pitch / 4) + 255) / 256;
+            if (blocks >= (int64_t)1 << 31) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many scales");
+            hipLaunchKernelGGL(k_pad_scales, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, from, rows, nblk, to, (int)pitch);
+            PV_HIP(ctx, hipGetLastError());
+            return PV_OK;
+        };
+        pv_status st = words(w_scales, out, ws);
+        if (st == PV_OK) st = words(x_scales, tokens, xs);
+        if (st != PV_OK) return st;
+        w.scales = ws;
+        x.scales = xs;
+    }
     return pv_for_dtype(y_type, [&](auto v) {
         using T = decltype(v);
-        return x_format == PV_MX_E2M1 ? launch<kE2M1, kE2M1>(ctx, w, x, nblk, static_cast<T *>(Y))
-                                      : launch<kE2M1, kE4M3>(ctx, w, x, nblk, static_cast<T *>(Y));
+        T *y = static_cast<T *>(Y);
+        if (x_format == PV_MX_E2M1) return launch<kE2M1, kE2M1>(ctx, c, w, x, nblk, pitch, partial, y);
+        if constexpr (std::is_same<T, float>::value) return PV_OK;      // (wide)
+        else return launch<kE2M1, kE4M3>(ctx, c, w, x, nblk, pitch, partial, y);
     });
 }
 
@@ -547,12 +720,15 @@ pv_status pv_launch_mx_product_grads(pv_ctx *ctx, int64_t tokens, int64_t out, i
 {
     const int64_t tp = padded(tokens), op = padded(out);
     const bool pad = dX && op != out;          // rows of dY that need an end
-    // in order: W^T, dY with padded rows | X^T, dY^T
+    const choice cx = choose<kBF16, kBF16>(in, tokens, (int)(op / 32)), cw = choose<kBF16, kBF16>(in, out, (int)(tp / 32));
+    // in order: the sums of either gradient | W^T, dY with padded rows | X^T, dY^T
+    const size_t sums = round16(dX && cx.partial > (dW ? cw.partial : 0) ? cx.partial : dW ? cw.partial : 0);
     const int64_t wt = dX ? in * op : 0, dyp = pad ? tokens * op : 0, xt = dW ? in * tp : 0, dyt = dW ? out * tp : 0;
     void *p;
-    pv_status st = pv_ops_scratch(ctx, (size_t)(wt + dyp + xt + dyt) * 2, &p);
+    pv_status st = pv_ops_scratch(ctx, sums + (size_t)(wt + dyp + xt + dyt) * 2, &p);
     if (st != PV_OK) return st;
-    pv_bf16 *WT = static_cast<pv_bf16 *>(p), *DYP = WT + wt, *XT = DYP + dyp, *DYT = XT + xt;
+    float *partial = static_cast<float *>(p);
+    pv_bf16 *WT = reinterpret_cast<pv_bf16 *>(static_cast<uint8_t *>(p) + sums), *DYP = WT + wt, *XT = DYP + dyp, *DYT = XT + xt;
     pv_timed t(ctx, PV_K_MX_PRODUCT);
     if (dX) {
         if ((st = transpose(ctx, kE2M1, w_codes, w_scales, out, in, WT)) != PV_OK) return st;
@@ -566,14 +742,14 @@ pv_status pv_launch_mx_product_grads(pv_ctx *ctx, int64_t tokens, int64_t out, i
         const operand w = plain(WT, in, op), x = plain(pad ? DYP : dY, tokens, op);
         st = pv_for_dtype(dx_type, [&](auto v) {
             using T = decltype(v);
-            return launch<kBF16, kBF16>(ctx, w, x, (int)(op / 32), static_cast<T *>(dX));
+            return launch<kBF16, kBF16>(ctx, cx, w, x, (int)(op / 32), 0, partial, static_cast<T *>(dX));
         });
         if (st != PV_OK) return st;
     }
     if (dW) {
         if ((st = transpose(ctx, x_format, x_codes, x_scales, tokens, in, XT)) != PV_OK) return st;
         if ((st = transpose(ctx, kBF16, dY, nullptr, tokens, out, DYT)) != PV_OK) return st;
-        st = launch<kBF16, kBF16>(ctx, plain(XT, in, tp), plain(DYT, out, tp), (int)(tp / 32), dW);
+        st = launch<kBF16, kBF16>(ctx, cw, plain(XT, in, tp), plain(DYT, out, tp), (int)(tp / 32), 0, partial, dW);
     }
     return st;
 }

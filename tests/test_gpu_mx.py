@@ -113,7 +113,9 @@ def operands(tokens, out, inn, fmt, seed):
 
 
 SHAPES = [(1, 1, 1), (1, 16, 32), (3, 5, 33), (1, 129, 4096), (16, 64, 128), (17, 100, 160), (31, 33, 100), (64, 256, 512),
-          (65, 250, 640), (130, 257, 1000), (200, 384, 2072), (256, 512, 1024), (300, 520, 1056), (513, 260, 96)]
+          (65, 250, 640), (130, 257, 1000), (200, 384, 2072), (256, 512, 1024), (300, 520, 1056), (513, 260, 96),
+          # sums in several parts, the last of them with part of a step
+          (17, 70, 4096), (40, 70, 5000), (129, 300, 8200)]
 
 
 def product_error(xs, ws, steps, cut=False):
@@ -145,6 +147,12 @@ def test_product(ctx, tokens, out, inn, fmt, dtype):
     assert far <= 2e-5 + ref.HALF_STEP[dtype]
 
 
+@pytest.mark.parametrize("fmt,dtype", [("e4m3", torch.bfloat16), ("e2m1", torch.float32), ("e4m3", torch.float32)], ids=str)
+@pytest.mark.parametrize("tokens,out,inn", [(2100, 4203, 300), (4097, 2049, 1024)])
+def test_product_in_large_tiles(ctx, tokens, out, inn, fmt, dtype):
+    test_product(ctx, tokens, out, inn, fmt, dtype)
+
+
 @pytest.mark.parametrize("fmt", ["e2m1", "e4m3"])
 @pytest.mark.parametrize("tokens,out,inn", [(1, 64, 256), (40, 70, 288), (257, 300, 544)])
 def test_a_block_that_is_nan_reaches_its_row_and_nothing_else(ctx, tokens, out, inn, fmt):
@@ -174,7 +182,8 @@ def test_product_of_scales_far_apart(ctx, fmt, dtype, scale):
 @pytest.mark.parametrize("dx_type", [torch.bfloat16, torch.float32], ids=str)
 @pytest.mark.parametrize("fmt", ["e2m1", "e4m3"])
 @pytest.mark.parametrize("tokens,out,inn", [(1, 1, 1), (2, 32, 32), (5, 33, 70), (64, 64, 64), (33, 130, 96), (100, 257, 300),
-                                            (256, 256, 512), (300, 200, 520), (129, 512, 384)])
+                                            (256, 256, 512), (300, 200, 520), (129, 512, 384), (40, 4100, 70), (4100, 40, 70),
+                                            (70, 4203, 2100)])
 def test_product_grads(ctx, tokens, out, inn, fmt, dx_type):
     xc, xs, wc, ws = operands(tokens, out, inn, fmt, seed=tokens * 3 + out + inn)
     dy = torch.randn(tokens, out, generator=gen(9)).to(torch.bfloat16)
