@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 from dataclasses import dataclass
-from functools import cached_property
+from functools import cached_property, lru_cache
 from pathlib import Path
 
 import torch
@@ -149,6 +149,7 @@ def _mx_format(fmt) -> int:
     return MX_FORMATS[fmt]
 
 
+@lru_cache(maxsize=1024)
 def mx_shapes(rows: int, cols: int, fmt: str):
     """Shapes of the codes and the scales (both uint8) of a [rows, cols] matrix."""
     nblk = -(-cols // MX_BLOCK)
@@ -316,37 +317,41 @@ class PVContext:
 
     # ---- operators around the V step --------------------------------------
     def _tensor(self, t, dtype, shape, what: str, allow_none: bool = False):
-        """Address of a dense tensor of this device, type(s) and shape."""
+        """Address of a dense tensor of this device, type (or one of several) and shape."""
         if t is None and allow_none:
             return None
-        types = dtype if isinstance(dtype, tuple) else (dtype,)
+        # the checks of a call cost as much as a small kernel: those that pass are few and cheap
+        if (isinstance(t, torch.Tensor) and (t.dtype is dtype or (dtype is _DTYPES and t.dtype in dtype)) and t.shape == shape
+                and t.get_device() == self.device and t.is_contiguous()):
+            return t.data_ptr()
+        types = tuple(dtype) if dtype is _DTYPES else (dtype,)
         if isinstance(t, torch.Tensor) and t.dtype not in types:
             raise TypeError(f"{what} must be {' or '.join(map(str, types))}, got {t.dtype}")
         ptr = _dev_ptr(t, getattr(t, "dtype", None), what)
-        if t.device.index != self.device:
+        if t.get_device() != self.device:
             raise ValueError(f"{what} is on {t.device}, the context on device {self.device}")
         if tuple(t.shape) != tuple(shape):
             raise ValueError(f"{what} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
         return ptr
 
-    def _coded(self, rows: int, cols: int, fmt: str, codes, scales, what: str = "", allow_none: bool = False):
-        shapes = mx_shapes(rows, cols, fmt)
-        return [self._tensor(t, torch.uint8, s, what + n, allow_none)
-                for t, s, n in ((codes, shapes[0], "codes"), (scales, shapes[1], "scales"))]
+    def _coded(self, rows: int, cols: int, fmt: str, codes, scales, of: str = "", allow_none: bool = False):
+        of_codes, of_scales = mx_shapes(rows, cols, fmt)
+        return (self._tensor(codes, torch.uint8, of_codes, of + "codes", allow_none),
+                self._tensor(scales, torch.uint8, of_scales, of + "scales", allow_none))
 
     def pv_quantize_mx(self, rows: int, cols: int, fmt: str, X, codes, scales):
-        x = self._tensor(X, tuple(_DTYPES), (rows, cols), "X")
+        x = self._tensor(X, _DTYPES, (rows, cols), "X")
         self._check(self._lib.pv_quantize_mx(self._h, int(rows), int(cols), _mx_format(fmt), _DTYPES[X.dtype], x,
                                              *self._coded(rows, cols, fmt, codes, scales)))
 
     def pv_dequantize_mx(self, rows: int, cols: int, fmt: str, codes, scales, out):
-        o = self._tensor(out, tuple(_DTYPES), (rows, cols), "out")
+        o = self._tensor(out, _DTYPES, (rows, cols), "out")
         self._check(self._lib.pv_dequantize_mx(self._h, int(rows), int(cols), _mx_format(fmt),
                                                *self._coded(rows, cols, fmt, codes, scales), _DTYPES[out.dtype], o))
 
     def pv_mx_product(self, tokens: int, out_features: int, in_features: int, x_format: str, x_codes, x_scales,
                       w_codes, w_scales, Y):
-        y = self._tensor(Y, tuple(_DTYPES), (tokens, out_features), "Y")
+        y = self._tensor(Y, _DTYPES, (tokens, out_features), "Y")
         self._check(self._lib.pv_mx_product(
             self._h, int(tokens), int(out_features), int(in_features), _mx_format(x_format),
             *self._coded(tokens, in_features, x_format, x_codes, x_scales, "x_"),
@@ -354,7 +359,7 @@ class PVContext:
 
     def pv_mx_product_grads(self, tokens: int, out_features: int, in_features: int, x_format: str, x_codes, x_scales,
                             w_codes, w_scales, dY, dX=None, dW=None):
-        dx = self._tensor(dX, tuple(_DTYPES), (tokens, in_features), "dX", allow_none=True)
+        dx = self._tensor(dX, _DTYPES, (tokens, in_features), "dX", allow_none=True)
         self._check(self._lib.pv_mx_product_grads(
             self._h, int(tokens), int(out_features), int(in_features), _mx_format(x_format),
             *self._coded(tokens, in_features, x_format, x_codes, x_scales, "x_", allow_none=dW is None),
@@ -365,7 +370,7 @@ class PVContext:
 
     def pv_rms_norm(self, rows: int, cols: int, x, residual, weight, eps: float, h=None, y=None, fmt: str = "e4m3",
                     codes=None, scales=None, rstd=None):
-        xp = self._tensor(x, tuple(_DTYPES), (rows, cols), "x")
+        xp = self._tensor(x, _DTYPES, (rows, cols), "x")
         same = lambda t, what: self._tensor(t, x.dtype, (rows, cols), what, allow_none=True)  # noqa: E731
         c, s = self._coded(rows, cols, fmt, codes, scales, allow_none=True)
         self._check(self._lib.pv_rms_norm(
@@ -374,7 +379,7 @@ class PVContext:
             _mx_format(fmt), c, s, self._tensor(rstd, torch.float32, (rows,), "rstd", allow_none=True)))
 
     def pv_rms_norm_backward(self, rows: int, cols: int, dy, dh, h, weight, rstd, dx=None, dweight=None):
-        g = self._tensor(dy, tuple(_DTYPES), (rows, cols), "dy")
+        g = self._tensor(dy, _DTYPES, (rows, cols), "dy")
         same = lambda t, what, none: self._tensor(t, dy.dtype, (rows, cols), what, allow_none=none)  # noqa: E731
         self._check(self._lib.pv_rms_norm_backward(
             self._h, int(rows), int(cols), _DTYPES[dy.dtype], g, same(dh, "dh", True), same(h, "h", False),
@@ -385,12 +390,12 @@ class PVContext:
         """Address and row stride of [rows, vocab] whose rows are dense."""
         if t is None:
             return None, vocab
-        types = dtype if isinstance(dtype, tuple) else (dtype,)
+        types = tuple(dtype) if dtype is _DTYPES else (dtype,)
         if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in types:
             raise TypeError(f"{what} must be a CUDA tensor of {' or '.join(map(str, types))}")
-        if t.device.index != self.device:
+        if t.get_device() != self.device:
             raise ValueError(f"{what} is on {t.device}, the context on device {self.device}")
-        if tuple(t.shape) != (rows, vocab):
+        if t.shape != (rows, vocab):
             raise ValueError(f"{what} must have the shape {(rows, vocab)}, got {tuple(t.shape)}")
         ld = t.stride(0) if rows > 1 else vocab
         if (vocab > 1 and t.stride(1) != 1) or ld < vocab:
@@ -406,7 +411,7 @@ class PVContext:
         row = lambda t, what, none: self._tensor(t, torch.float32, (rows,), what, allow_none=none)  # noqa: E731
         if logits is None:
             raise TypeError("logits is None")
-        z, ld = self._strided(logits, tuple(_DTYPES), rows, vocab, "logits")
+        z, ld = self._strided(logits, _DTYPES, rows, vocab, "logits")
         g, grad_ld = self._strided(grad, logits.dtype, rows, vocab, "grad")
         ids, top = self._teacher(rows, k, teacher_ids, teacher_logits)
         self._check(self._lib.pv_distill_topk(
@@ -418,7 +423,7 @@ class PVContext:
         row = lambda t, what: self._tensor(t, torch.float32, (rows,), what)  # noqa: E731
         if logits is None or grad is None:
             raise TypeError("logits or grad is None")
-        z, ld = self._strided(logits, tuple(_DTYPES), rows, vocab, "logits")
+        z, ld = self._strided(logits, _DTYPES, rows, vocab, "logits")
         g, grad_ld = self._strided(grad, logits.dtype, rows, vocab, "grad")
         ids, top = self._teacher(rows, k, teacher_ids, teacher_logits)
         self._check(self._lib.pv_distill_topk_backward(

@@ -45,8 +45,7 @@ __device__ __forceinline__ int piece_of(int step, int j, int q)
 }
 
 template <bool WIDE, int KIND>
-__device__ __forceinline__ void load_part(part<KIND> &p, const uint8_t *row, const uint8_t *scale_row,
-                                          int step, int q, int nblk)
+__device__ __forceinline__ void load_part(part<KIND> &p, const uint8_t *row, int step, int q, int nblk)
 {
 #pragma unroll
     for (int j = 0; j < part<KIND>::chunks; ++j) {
@@ -56,8 +55,23 @@ __device__ __forceinline__ void load_part(part<KIND> &p, const uint8_t *row, con
         p.c[j] = pv_u4{0u, 0u, 0u, 0u};
         if (block < nblk) p.c[j] = *reinterpret_cast<const pv_u4 *>(row + (int64_t)piece * 16);
     }
-    p.scale = 127u;
-    if (step * 4 + q < nblk) p.scale = scale_row[step * 4 + q];
+}
+
+// scale bytes of the blocks of four steps, this lane group's block of each in the low byte; behind the row's end: 0
+__device__ __forceinline__ pv_u4 load_scales(const uint8_t *scale_row, int step, int q, int nblk)
+{
+    typedef pv_u4 loose __attribute__((aligned(1)));
+    pv_u4 v = {0u, 0u, 0u, 0u};
+    if (step * 4 + 16 <= nblk) {
+        v = *reinterpret_cast<const loose *>(scale_row + step * 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = v[i] >> (8 * q) & 255u;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if ((step + i) * 4 + q < nblk) v[i] = scale_row[(step + i) * 4 + q];
+    }
+    return v;
 }
 
 // eight values, 8 j .. 8 j + 7 of the lane's block, as bf16
@@ -118,56 +132,49 @@ __device__ __forceinline__ void store_four(T *y, int left, bool whole, f4v v)
         if (i < left) y[i] = (T)v[i];
 }
 
-// 16 rows of W and 16 * NT of X a block, straight from memory to registers; the four waves take every fourth step of 128
-// values and meet in LDS.
-template <bool WIDE, int WK, int XK, int NT, class T>
-__global__ __launch_bounds__(256) void k_product_direct(operand w, operand x, int nblk, T *__restrict__ Y, int wtiles)
+// Few tokens: 16 rows of W and 16 of X a block, straight from memory to registers.  Bound by W's bytes and by the way there: the
+// waves take four steps of 128 values each in turn, ask for all of them before they multiply the first, and meet in LDS.
+// Eight waves where there are no more than two blocks a compute unit, else four (1 token, us with 4 | 8 waves: 4096 -> 11008
+// 8.3 | 10.2, 14336 -> 4096 13.1 | 10.4; 24 and 31 MB of W, where a launch that does next to nothing takes 3).
+constexpr int kBatch = 4;
+
+template <bool WIDE, int WK, int XK, int WAVES, class T>
+__global__ __launch_bounds__(WAVES * 64) void k_product_direct(operand w, operand x, int nblk, T *__restrict__ Y, int wtiles)
 {
-    __shared__ f4v sums[3][NT][64];
+    __shared__ f4v sums[WAVES - 1][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int q = lane >> 4, r = lane & 15;
-    const int wt = blockIdx.x % wtiles, xt = blockIdx.x / wtiles;
-    const int o0 = wt * 16, t0 = xt * 16 * NT;
+    const int o0 = blockIdx.x % wtiles * 16, t0 = blockIdx.x / wtiles * 16;
     const int steps = (nblk + 3) / 4;
     // rows past the end repeat the last one; their results are not stored
-    const int wrow = min(o0 + r, w.rows - 1);
+    const int wrow = min(o0 + r, w.rows - 1), xrow = min(t0 + r, x.rows - 1);
     const uint8_t *wp = w.codes + wrow * w.pitch, *ws = w.scales + (int64_t)wrow * nblk;
-    const uint8_t *xp[NT], *xs[NT];
+    const uint8_t *xp = x.codes + xrow * x.pitch, *xs = x.scales + (int64_t)xrow * nblk;
+    f4v acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    static_assert(kBatch == 4, "as many steps as load_scales brings");
+    for (int s = wave * kBatch; s < steps; s += WAVES * kBatch) {
+        part<WK> a[kBatch];
+        part<XK> b[kBatch];
+        const pv_u4 as = load_scales(ws, s, q, nblk), bs = load_scales(xs, s, q, nblk);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int xrow = min(t0 + n * 16 + r, x.rows - 1);
-        xp[n] = x.codes + xrow * x.pitch;
-        xs[n] = x.scales + (int64_t)xrow * nblk;
-    }
-    f4v acc[NT];
+        for (int i = 0; i < kBatch; ++i) {           // behind the last step: zeros
+            load_part<WIDE>(a[i], wp, s + i, q, nblk);
+            load_part<WIDE>(b[i], xp, s + i, q, nblk);
+            a[i].scale = as[i];
+            b[i].scale = bs[i];
+        }
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[n] = f4v{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = wave; s < steps; s += 4) {
-        part<WK> a;
-        part<XK> b[NT];
-        load_part<WIDE>(a, wp, ws, s, q, nblk);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) load_part<WIDE>(b[n], xp[n], xs[n], s, q, nblk);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[n] = multiply<WIDE>(a, b[n], acc[n]);
+        for (int i = 0; i < kBatch; ++i) acc = multiply<WIDE>(a[i], b[i], acc);
     }
     // the last instructions run here, by every lane, not inside a branch that stores their results
-#pragma unroll
-    for (int n = 0; n < NT; ++n) asm volatile("" : "+v"(acc[n]));
-    if (wave) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) sums[wave - 1][n][lane] = acc[n];
-    }
+    asm volatile("" : "+v"(acc));
+    if (wave) sums[wave - 1][lane] = acc;
     __syncthreads();
     if (wave) return;
-    const bool vec = (w.rows & 3) == 0;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-#pragma unroll
-        for (int i = 0; i < 3; ++i) acc[n] += sums[i][n][lane];
-        const int t = t0 + n * 16 + r, o = o0 + q * 4;
-        if (t < x.rows && o < w.rows) store_four(Y + (int64_t)t * w.rows + o, w.rows - o, vec, acc[n]);
-    }
+    for (int i = 0; i < WAVES - 1; ++i) acc += sums[i][lane];
+    const int t = t0 + r, o = o0 + q * 4;
+    if (t < x.rows && o < w.rows) store_four(Y + (int64_t)t * w.rows + o, w.rows - o, (w.rows & 3) == 0, acc);
 }
 
 // ---------------------------------------------------------------- tiles through LDS
@@ -601,13 +608,15 @@ pv_status launch_tiled(pv_ctx *ctx, const operand &w, const operand &x, tiling p
     return PV_OK;
 }
 
-template <bool WIDE, int WK, int XK, int NT, class T>
+template <bool WIDE, int WK, int XK, class T>
 pv_status launch_direct(pv_ctx *ctx, const operand &w, const operand &x, int nblk, T *Y)
 {
     const int wtiles = (w.rows + 15) / 16;
-    const int64_t blocks = (int64_t)wtiles * ((x.rows + 16 * NT - 1) / (16 * NT));
+    const int64_t blocks = (int64_t)wtiles * ((x.rows + 15) / 16);
     if (blocks >= (int64_t)1 << 31) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many tiles of the product");
-    hipLaunchKernelGGL((k_product_direct<WIDE, WK, XK, NT, T>), dim3((unsigned)blocks), dim3(256), 0, ctx->stream, w, x, nblk, Y, wtiles);
+    const bool few = blocks <= 512;
+    const auto k = few ? k_product_direct<WIDE, WK, XK, 8, T> : k_product_direct<WIDE, WK, XK, 4, T>;
+    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(few ? 512 : 256), 0, ctx->stream, w, x, nblk, Y, wtiles);
     PV_HIP(ctx, hipGetLastError());
     return PV_OK;
 }
@@ -668,8 +677,8 @@ pv_status pv_launch_mx_product(pv_ctx *ctx, int64_t tokens, int64_t out, int64_t
         return pv_for_dtype(y_type, [&](auto v) {
             using T = decltype(v);
             T *y = static_cast<T *>(Y);
-            if (x_format == PV_MX_E2M1) return launch_direct<false, kE2M1, kE2M1, 1>(ctx, w, x, nblk, y);
-            return launch_direct<std::is_same<T, float>::value, kE2M1, kE4M3, 1>(ctx, w, x, nblk, y);
+            if (x_format == PV_MX_E2M1) return launch_direct<false, kE2M1, kE2M1>(ctx, w, x, nblk, y);
+            return launch_direct<std::is_same<T, float>::value, kE2M1, kE4M3>(ctx, w, x, nblk, y);
         });
     }
     // scratch: both sides as bf16, or scales with rows of whole words; the splits' sums
