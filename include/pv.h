@@ -379,6 +379,8 @@ pv_status pv_rms_norm_backward(pv_ctx *ctx, int64_t rows, int64_t cols, pv_dtype
  * counts twice.  row_weight f32 [rows] (NULL: 1): a row of weight 0 is not read; its loss, lse and
  * gradient are 0.  A row without an entry, or whose entries are all -infinity, has loss 0 and
  * gradient 0 (lse is still written).  An entry with p_j == 0 adds nothing whatever q is there.
+ * Places of logit -infinity have q = 0; a row of equal logits is uniform, also one of the type's
+ * lowest value; NaN, +infinity or nothing but -infinity in a row makes its results NaN.
  * logits [rows, vocab], row stride ld >= vocab elements; grad alike with grad_ld, and may be logits
  * (same pointer and stride): behind a row's vocab elements nothing is read or written.
  * teacher_ids i32 [rows, k], teacher_logits f32 [rows, k].  0 <= k <= 1024, 1 <= vocab <= 2^20,

@@ -4,15 +4,15 @@
 // Bound by HBM: the logits in, the gradient out, 2 or 4 bytes an entry each.  A block takes a row, and the
 // row stays in its registers between the sum and the gradient where they hold it; the exponentials are formed twice
 // instead of being kept, at 16 a clock and compute unit they cost a fraction of the bytes.
-// The teacher's entries are k places of the row: a bit per place marks them in LDS, the sweep that writes the gradient
-// leaves marked places out, and the first entry of each id writes its place, less the sum of the entries with that id
-// in the order of the list - one writer a place, no atomics on sums, and the same bits every time.
+// The teacher's entries are k places of the row.  The sweep writes all of the row as if there were none; once its stores are
+// done the first entry of each id writes its place again, less the sum of the entries with that id in the order of the
+// list: one writer a place, no atomics on sums, the same bits every time.  (A sweep that leaves the places out
+// splits a store of 16 bytes into single elements wherever one lies: 2048 x 32000 with 256 entries 76 us.)  A bit per place in
+// LDS tells whether any place has two entries; only then are the lists compared.
 #include "pv_ops.h"
 
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kWaves = kThreads / 64;
 constexpr float kLog2e = 1.44269504088896340736f;
 
 template <class T>
@@ -22,6 +22,26 @@ struct unit_of {                                  // 16 bytes of a row, at any e
     typedef raw type __attribute__((aligned(sizeof(T))));
 };
 
+// two values over a block, with one barrier
+template <int WAVES, class F>
+__device__ __forceinline__ void reduce_two(float &a, float &b, float *part, F f)
+{
+    a = pv_wave_reduce(a, f);
+    b = pv_wave_reduce(b, f);
+    if ((threadIdx.x & 63) == 0) {
+        part[threadIdx.x >> 6] = a;
+        part[WAVES + (threadIdx.x >> 6)] = b;
+    }
+    __syncthreads();
+    a = part[0];
+    b = part[WAVES];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) {
+        a = f(a, part[w]);
+        b = f(b, part[WAVES + w]);
+    }
+}
+
 struct args {
     const int32_t *ids;
     const float *top, *row_weight, *lse_in;
@@ -29,52 +49,56 @@ struct args {
     int64_t ld, grad_ld;
     int vocab, k;
     float t;
+    unsigned pieces;         // blocks a row (backward)
 };
 
-// NV > 0: the row lies in NV units a thread.  NV == 0: the row is read again for the gradient.
-// LSE: the sum is given (the backward call), only the gradient is formed.
-template <class T, int NV, bool LSE>
-__global__ __launch_bounds__(kThreads) void k_distill(const T *logits, T *grad, args a)
+// NV > 0: the row lies in NV units a thread.  NV == 0: it passes by, with a running largest value and sum in each thread, and
+// is read again for the gradient if there is one.
+// LSE: the sum is given (the backward call), only the gradient is formed, by a block for every NV units a thread of a row.
+template <class T, int THREADS, int NV, bool LSE>
+__global__ __launch_bounds__(THREADS) void k_distill(const T *logits, T *grad, args a)
 {
-    constexpr int U = unit_of<T>::n;
+    constexpr int U = unit_of<T>::n, kWaves = THREADS / 64;
+    constexpr float kNone = -__builtin_inff();
     typedef typename unit_of<T>::raw raw;
     typedef typename unit_of<T>::type loose;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    float *part = reinterpret_cast<float *>(lds);                     // [2][kWaves]
-    float *p = part + 2 * kWaves;                                     // [k] the teacher's probabilities
+    float *p = reinterpret_cast<float *>(lds);                        // [k] the teacher's logits by the temperature
     float *zt = p + a.k;                                              // [k] the logits in their places
     int *id = reinterpret_cast<int *>(zt + a.k);                      // [k] their places, -1: none
     unsigned *mark = reinterpret_cast<unsigned *>(id + a.k);          // [ceil(vocab / 32)] places of the row
+    __shared__ float part[3][2 * kWaves];
+    __shared__ int s_twice;                                           // some place has two entries
 
-    __shared__ int twice;                                             // some place has two entries
-    const int64_t row = blockIdx.x;
     const int tid = threadIdx.x, V = a.vocab, k = a.k;
+    const int64_t row = LSE ? blockIdx.x / a.pieces : blockIdx.x;
+    const int first = LSE ? (int)(blockIdx.x % a.pieces) * (NV * THREADS) : 0;      // unit of this block
     const T *z = logits + row * a.ld;
     T *g = grad ? grad + row * a.grad_ld : nullptr;
     const float c = a.row_weight ? a.row_weight[row] : 1.0f;
-    const int units = (V + U - 1) / U;
+    const int units = LSE ? min((V + U - 1) / U, first + NV * THREADS) : (V + U - 1) / U;
 
     auto load = [&](int unit) {
         raw r;
         if ((unit + 1) * U <= V) return (raw)*reinterpret_cast<const loose *>(z + unit * U);
 #pragma unroll
-        for (int i = 0; i < U; ++i) r[i] = unit * U + i < V ? z[unit * U + i] : (T)(-__builtin_inff());
+        for (int i = 0; i < U; ++i) r[i] = unit * U + i < V ? z[unit * U + i] : (T)kNone;
         return r;
     };
-    auto store = [&](int unit, const raw &r, unsigned skip) {
-        if (skip == 0 && (unit + 1) * U <= V) {
+    auto store = [&](int unit, const raw &r) {
+        if ((unit + 1) * U <= V) {
             *reinterpret_cast<loose *>(g + unit * U) = r;
             return;
         }
 #pragma unroll
         for (int i = 0; i < U; ++i)
-            if (unit * U + i < V && !(skip >> i & 1)) g[unit * U + i] = r[i];
+            if (unit * U + i < V) g[unit * U + i] = r[i];
     };
 
     if (c == 0.0f) {
         const raw zero = {};
         if (g)
-            for (int unit = tid; unit < units; unit += kThreads) store(unit, zero, 0);
+            for (int unit = first + tid; unit < units; unit += THREADS) store(unit, zero);
         if (tid == 0 && !LSE) {
             a.loss[row] = 0.0f;
             if (a.lse) a.lse[row] = 0.0f;
@@ -86,130 +110,149 @@ __global__ __launch_bounds__(kThreads) void k_distill(const T *logits, T *grad, 
     if constexpr (NV > 0) {
 #pragma unroll
         for (int u = 0; u < NV; ++u)
-            if (u * kThreads + tid < units) v[u] = load(u * kThreads + tid);
+            if (first + u * THREADS + tid < units) v[u] = load(first + u * THREADS + tid);
     }
-    // the teacher's entries, while the row is on its way: the first wave forms their softmax
-    const float inv_t = 1.0f / a.t;
-    float log_sum_u = 0.0f, max_u = -__builtin_inff();
+    // the teacher's entries, while the row is on its way: a thread each, or more
+    const float inv_t = 1.0f / a.t, scale = kLog2e * inv_t;
+    float top = kNone, total = 0.0f, max_u = kNone, sum_u = 0.0f;
+    for (int j = tid; j < k; j += THREADS) {
+        const int i = a.ids[row * k + j];
+        const bool in = i >= 0 && i < V;
+        const float u = in ? a.top[row * k + j] * inv_t : kNone;
+        id[j] = in ? i : -1;
+        p[j] = u;
+        zt[j] = in ? (float)z[i] : 0.0f;
+        max_u = fmaxf(max_u, u);
+    }
     if (g)
-        for (int w = tid; w < (V + 31) / 32; w += kThreads) mark[w] = 0;
-    if (tid == 0) twice = 0;
-    if (tid < 64) {
-        for (int j = tid; j < k; j += 64) {
-            const int i = a.ids[row * k + j];
-            const bool in = i >= 0 && i < V;
-            const float u = in ? a.top[row * k + j] * inv_t : -__builtin_inff();
-            id[j] = in ? i : -1;
-            p[j] = u;
-            zt[j] = in ? (float)z[i] : 0.0f;
-            max_u = fmaxf(max_u, u);
-        }
-        max_u = pv_wave_reduce(max_u, pv_max{});
-        float sum = 0.0f;
-        for (int j = tid; j < k; j += 64) sum += id[j] >= 0 && max_u > -__builtin_inff() ? expf(p[j] - max_u) : 0.0f;
-        sum = pv_wave_reduce(sum, pv_add{});
-        log_sum_u = logf(sum);                    // -inf: no entry
-    }
-
-    // q_v = exp2(z_v * scale - shift)
-    const float scale = kLog2e * inv_t;
-    float top = -__builtin_inff(), lse, total = 0.0f;
-    if constexpr (LSE) {
-        lse = a.lse_in[row];
-        __syncthreads();          // the marks are clear
-    } else {
-        auto largest = [&](const raw &r) {
+        for (int w = tid; w < (V + 31) / 32; w += THREADS) mark[w] = 0;
+    if (tid == 0) s_twice = 0;
+    if constexpr (!LSE && NV > 0) {
 #pragma unroll
-            for (int i = 0; i < U; ++i) top = fmaxf(top, (float)r[i]);
-        };
-        if constexpr (NV > 0) {
+        for (int u = 0; u < NV; ++u)
+            if (u * THREADS + tid < units) {
 #pragma unroll
-            for (int u = 0; u < NV; ++u)
-                if (u * kThreads + tid < units) largest(v[u]);
-        } else {
-            for (int unit = tid; unit < units; unit += kThreads) largest(load(unit));
-        }
-        top = pv_block_reduce<kThreads>(top, part, pv_max{});
-        auto add = [&](const raw &r, int unit) {
-#pragma unroll
-            for (int i = 0; i < U; ++i) total += __builtin_amdgcn_exp2f(((float)r[i] - top) * scale);
-        };
-        if constexpr (NV > 0) {
-#pragma unroll
-            for (int u = 0; u < NV; ++u)
-                if (u * kThreads + tid < units) add(v[u], u * kThreads + tid);
-        } else {
-            for (int unit = tid; unit < units; unit += kThreads) add(load(unit), unit);
-        }
-        total = pv_block_reduce<kThreads>(total, part + kWaves, pv_add{});
-        lse = top * inv_t + logf(total);
-    }
-
-    // the loss, and the entries' probabilities in place of their logits
-    if (tid < 64) {
-        const bool any = log_sum_u != -__builtin_inff();
-        float loss = 0.0f;
-        for (int j = tid; j < k; j += 64) {
-            const float log_p = p[j] - max_u - log_sum_u;
-            const float pj = any && id[j] >= 0 ? expf(log_p) : 0.0f;
-            if (!LSE && pj != 0.0f) {
-                const float log_q = (zt[j] - top) * inv_t - logf(total);
-                loss = fmaf(pj, log_p - log_q, loss);
+                for (int i = 0; i < U; ++i) top = fmaxf(top, (float)v[u][i]);
             }
-            p[j] = pj;
-            if (g && pj != 0.0f) {
-                const unsigned bit = 1u << (id[j] & 31);
-                if (atomicOr(&mark[id[j] >> 5], bit) & bit) twice = 1;
-            }
+    } else if constexpr (!LSE) {
+#pragma unroll 2
+        for (int unit = tid; unit < units; unit += THREADS) {
+            const raw r = load(unit);
+            float m = top;
+#pragma unroll
+            for (int i = 0; i < U; ++i) m = fmaxf(m, (float)r[i]);
+            total *= top == m ? 1.0f : __builtin_amdgcn_exp2f((top - m) * scale);
+            top = m;
+            // (as long as nothing but -infinity has passed, m is no number to subtract)
+#pragma unroll
+            for (int i = 0; i < U; ++i) total += (float)r[i] == kNone ? 0.0f : __builtin_amdgcn_exp2f(((float)r[i] - m) * scale);
         }
-        if constexpr (!LSE) {
-            loss = pv_wave_reduce(loss, pv_add{});
-            if (tid == 0) {
-                a.loss[row] = any ? c * a.t * a.t * loss : 0.0f;
-                if (a.lse) a.lse[row] = lse;
-            }
-        }
-        if (tid == 0) part[0] = any ? c * a.t : 0.0f;
     }
-    if (!g) return;
-    __syncthreads();
-    const float factor = part[0], inv_total = 1.0f / total;
-
-    auto q_of = [&](float x) {
-        // forward: relative to the largest, as the sum was taken; backward: from the log of the sum
-        if constexpr (LSE) return __builtin_amdgcn_exp2f(fmaf(x, inv_t, -lse) * kLog2e);
-        return __builtin_amdgcn_exp2f((x - top) * scale) * inv_total;
+    const float own_top = top;
+    reduce_two<kWaves>(top, max_u, part[0], pv_max{});
+    // the marks are clear, and the largest of either are known
+    for (int j = tid; j < k; j += THREADS) {
+        if (id[j] < 0) continue;
+        const float u = p[j];
+        sum_u += max_u > kNone || u != u ? expf(u - max_u) : 0.0f;
+        if (g) {
+            const unsigned bit = 1u << (id[j] & 31);
+            if (atomicOr(&mark[id[j] >> 5], bit) & bit) s_twice = 1;
+        }
+    }
+    // q_v = exp2(z_v * scale - shift) / total, one operation an exponent; a rounded shift is the same in q and in the total.  A largest
+    // logit near the ends of float32 (a row masked by the type's lowest value) is subtracted first: its shift is not finite.
+    const float shift = top * scale;
+    const bool far = !(fabsf(top) < 1e30f);
+    auto weight = [&](float x, auto is_far) {
+        return __builtin_amdgcn_exp2f(decltype(is_far)::value ? (x - top) * scale : fmaf(x, scale, -shift));
     };
-    // the entries' own places, once each
-    if (tid < k && p[tid] != 0.0f) {
-        int place = id[tid];
-        float sum = p[tid];
-        if (twice) {
-            sum = 0.0f;
+    if constexpr (!LSE && NV > 0) {
+        auto sum = [&](auto is_far) {
+#pragma unroll
+            for (int u = 0; u < NV; ++u)
+                if (u * THREADS + tid < units) {
+#pragma unroll
+                    for (int i = 0; i < U; ++i) total += weight((float)v[u][i], is_far);
+                }
+        };
+        if (far) sum(std::true_type{});
+        else sum(std::false_type{});
+    } else if constexpr (!LSE) {
+        total *= __builtin_amdgcn_exp2f((own_top - top) * scale);
+    }
+    reduce_two<kWaves>(total, sum_u, part[1], pv_add{});
+    // p_j = exp(u_j - max_u - log_sum_u); q_v as above, or exp(z_v / t - lse) with the sum given
+    const bool any = sum_u != 0.0f;               // (of the largest entry's 1, unless there is none)
+    const float log_sum_u = logf(sum_u), inv_total = 1.0f / total, lse = LSE ? a.lse_in[row] : 0.0f;
+    const float factor = any ? c * a.t : 0.0f;
+    auto p_of = [&](int j) { return any && id[j] >= 0 ? expf(p[j] - max_u - log_sum_u) : 0.0f; };
+    const float factor_q = LSE ? factor : factor * inv_total;
+    auto grad_q = [&](float x, auto is_far) {
+        if constexpr (LSE) return factor_q * __builtin_amdgcn_exp2f(fmaf(x, inv_t, -lse) * kLog2e);
+        return factor_q * weight(x, is_far);
+    };
+    if (g) {
+        auto sweep = [&](auto is_far) {
+            auto emit = [&](int unit, const raw &r) {
+                raw o;
+#pragma unroll
+                for (int i = 0; i < U; ++i) o[i] = (T)grad_q((float)r[i], is_far);
+                store(unit, o);
+            };
+            if constexpr (NV > 0) {
+#pragma unroll
+                for (int u = 0; u < NV; ++u)
+                    if (first + u * THREADS + tid < units) emit(first + u * THREADS + tid, v[u]);
+            } else {
+                for (int unit = tid; unit < units; unit += THREADS) emit(unit, load(unit));
+            }
+        };
+        if (factor == 0.0f) {
+            const raw zero = {};
+            for (int unit = first + tid; unit < units; unit += THREADS) store(unit, zero);
+        } else if (!LSE && far) {
+            sweep(std::true_type{});
+        } else {
+            sweep(std::false_type{});
+        }
+    }
+    if constexpr (!LSE) {
+        // where the rounded shift was subtracted, the total is off by what it was rounded by (of a register row; 6e-8 of the largest logit)
+        const float log_total = logf(total) - (NV == 0 || far ? 0.0f : fmaf(top, scale, -shift) * 0.69314718055994530942f);
+        float loss = 0.0f;
+        for (int j = tid; j < k; j += THREADS) {
+            const float pj = p_of(j);
+            if (pj != 0.0f) loss = fmaf(pj, ((p[j] - max_u - log_sum_u) - (zt[j] - top) * inv_t) + log_total, loss);
+        }
+        loss = pv_block_reduce<THREADS>(loss, part[2], pv_add{});
+        if (tid == 0) {
+            a.loss[row] = any ? c * a.t * a.t * loss : 0.0f;
+            if (a.lse) a.lse[row] = top * inv_t + log_total;
+        }
+    }
+    if (!g || factor == 0.0f) return;
+    // The entries' own places, once each, by the first entry of a place, over what the sweep left there: its stores are done when the
+    // waves meet.
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    for (int e = tid; e < k; e += THREADS) {
+        int place = id[e];
+        if (place < 0) continue;
+        float sum = 0.0f;
+        if (s_twice) {
             for (int j = 0; j < k; ++j)
-                if (id[j] == place && p[j] != 0.0f) {
-                    if (j < tid) {
+                if (id[j] == place) {
+                    if (j < e) {
                         place = -1;
                         break;
                     }
-                    sum += p[j];
+                    sum += p_of(j);
                 }
+        } else {
+            sum = p_of(e);
         }
-        if (place >= 0) g[place] = (T)(factor * (q_of(zt[tid]) - sum));
-    }
-    auto emit = [&](int unit, raw r) {
-        const unsigned word = mark[unit * U >> 5] >> (unit * U & 31) & ((1u << U) - 1);
-#pragma unroll
-        for (int i = 0; i < U; ++i) r[i] = factor != 0.0f ? (T)(factor * q_of((float)r[i])) : (T)0.0f;
-        store(unit, r, word);
-    };
-    if constexpr (NV > 0) {
-#pragma unroll
-        for (int u = 0; u < NV; ++u)
-            if (u * kThreads + tid < units) emit(u * kThreads + tid, v[u]);
-    } else {
-        // a place that an entry has written already (grad may be logits) is read and left out
-        for (int unit = tid; unit < units; unit += kThreads) emit(unit, load(unit));
+        if (place >= first * U && place < units * U) g[place] = (T)((far ? grad_q(zt[e], std::true_type{}) : grad_q(zt[e], std::false_type{})) - factor * sum);
     }
 }
 
@@ -219,30 +262,36 @@ pv_status pv_launch_distill(pv_ctx *ctx, int64_t rows, int64_t vocab, int k, int
                             const int32_t *ids, const float *top, float temperature, const float *row_weight,
                             float *loss, float *lse, const float *lse_in, void *grad, int64_t grad_ld)
 {
-    const args a = {ids, top, row_weight, lse_in, loss, lse, ld, grad_ld, (int)vocab, k, temperature};
-    const size_t lds = (2 * kWaves + 3 * (size_t)k) * 4 + (grad ? (size_t)((vocab + 31) / 32) * 4 : 0);
+    args a = {ids, top, row_weight, lse_in, loss, lse, ld, grad_ld, (int)vocab, k, temperature, 1};
+    const size_t lds = 3 * (size_t)k * 4 + (grad ? (size_t)((vocab + 31) / 32) * 4 : 0);
     pv_timed t(ctx, PV_K_DISTILL);
     return pv_for_dtype(type, [&](auto v) {
         using T = decltype(v);
-        const int units = (int)((vocab + unit_of<T>::n - 1) / unit_of<T>::n), nv = (units + kThreads - 1) / kThreads;
-        auto launch = [&](auto kernel) {
-            if (lds > 65536)
+        const int units = (int)((vocab + unit_of<T>::n - 1) / unit_of<T>::n);
+        auto launch = [&](auto kernel, int threads) {
+            const int64_t blocks = rows * a.pieces;
+            if (blocks >= (int64_t)1 << 31) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many rows of logits");
+            if (lds > 65536 - 1024)
                 PV_HIP(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-            hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(kThreads), lds, ctx->stream,
+            hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), lds, ctx->stream,
                                static_cast<const T *>(logits), static_cast<T *>(grad), a);
             PV_HIP(ctx, hipGetLastError());
             return PV_OK;
         };
-        auto pick = [&](auto given) {
-            constexpr bool LSE = decltype(given)::value;
-            if (nv <= 1) return launch(k_distill<T, 1, LSE>);
-            if (nv <= 2) return launch(k_distill<T, 2, LSE>);
-            if (nv <= 4) return launch(k_distill<T, 4, LSE>);
-            if (nv <= 8) return launch(k_distill<T, 8, LSE>);
-            if (nv <= 16) return launch(k_distill<T, 16, LSE>);
-            return launch(k_distill<T, 0, LSE>);
-        };
-        return lse_in ? pick(std::true_type{}) : pick(std::false_type{});
+        if (lse_in) {
+            const int threads = units <= 256 * 4 ? 256 : 512;
+            a.pieces = (unsigned)((units + threads * 4 - 1) / (threads * 4));
+            return threads == 256 ? launch(k_distill<T, 256, 4, true>, 256) : launch(k_distill<T, 512, 4, true>, 512);
+        }
+        // few threads a row, and many rows on a compute unit, as long as they hold theirs; the loss alone holds nothing
+        if (units <= 256) return launch(k_distill<T, 256, 1, false>, 256);
+        if (units <= 256 * 4) return launch(k_distill<T, 256, 4, false>, 256);
+        if (units <= 512 * 4) return launch(k_distill<T, 512, 4, false>, 512);
+        if (units <= 512 * 8) return launch(k_distill<T, 512, 8, false>, 512);
+        if (!grad) return launch(k_distill<T, 512, 0, false>, 512);
+        if (units <= 1024 * 8) return launch(k_distill<T, 1024, 8, false>, 1024);
+        if (units <= 1024 * 16) return launch(k_distill<T, 1024, 16, false>, 1024);
+        return launch(k_distill<T, 512, 0, false>, 512);
     });
 }

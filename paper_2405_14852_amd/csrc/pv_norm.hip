@@ -9,59 +9,76 @@ namespace {
 
 constexpr int kBlock = 256;
 
-// TPR threads share a row (64: four rows a block, no barrier; kBlock: one row a block), each with NV times eight values.
-template <class T, int TPR, int NV, int FMT>
-__global__ __launch_bounds__(kBlock) void k_rms_norm(const T *x, const T *residual, const float *__restrict__ weight,
-                                                     float eps, T *h, T *y, uint8_t *__restrict__ codes,
-                                                     uint8_t *__restrict__ scales, float *__restrict__ rstd_out,
-                                                     int64_t rows, int64_t cols, int nblk)
+// One row's outputs from its stored sum v (a thread's eight values of it)
+template <class T, int FMT>
+__device__ __forceinline__ void norm_out(const float (&v)[8], float rstd, const float (&w)[8], int valid, int unit, int units,
+                                         int64_t row, int64_t cols, T *y, uint8_t *codes, uint8_t *scales)
 {
-    __shared__ float part[kBlock / 64];
-    const int t = threadIdx.x % TPR;
-    const int64_t row = (int64_t)blockIdx.x * (kBlock / TPR) + threadIdx.x / TPR;
-    if (row >= rows) return;             // a whole wave, and a whole block where they meet in barriers
-    const int64_t base = row * cols;
-    const int units = nblk * 4;
-    // every load before the first store: the outputs may lie on the inputs, so the compiler keeps their order
-    float v[NV][8], r[NV][8];
+    float o[8];
 #pragma unroll
-    for (int u = 0; u < NV; ++u) {
-        const int unit = u * TPR + t, valid = (int)cols - unit * 8;
-        pv_load8(x + base + (int64_t)unit * 8, valid, v[u]);
-        if (residual) pv_load8(residual + base + (int64_t)unit * 8, valid, r[u]);
+    for (int i = 0; i < 8; ++i) o[i] = (v[i] * rstd) * w[i];
+    if (y) pv_store8(y + row * cols + (int64_t)unit * 8, valid, o);
+    if (codes && unit < units) {
+        const unsigned scale = pv_mx_scale<FMT>(pv_mx_largest(o));
+        const pv_u2 c = pv_mx_encode<FMT>(o, scale);
+        const int64_t at = row * units + unit;
+        if constexpr (FMT == PV_MX_E2M1) reinterpret_cast<unsigned *>(codes)[at] = c.x;
+        else reinterpret_cast<pv_u2 *>(codes)[at] = c;
+        if ((unit & 3) == 0) scales[at >> 2] = (uint8_t)scale;
     }
-    float sum = 0.0f;
+}
+
+// TPR threads share a row (64: kBlock / 64 rows a block, no barrier; else the block's), each with NV times eight values.  A block
+// goes from row to row, in steps of the grid, with its weights in registers and the next row already on its way while this
+// one is summed (8192 x 4096, bf16 to e4m3: 63.8 us with a wave a row and the weights read for each).
+template <class T, int TPR, int NV, int FMT>
+__global__ __launch_bounds__(TPR == 64 ? kBlock : TPR) void k_rms_norm(const T *x, const T *residual,
+                                                                       const float *__restrict__ weight, float eps, T *h,
+                                                                       T *y, uint8_t *__restrict__ codes,
+                                                                       uint8_t *__restrict__ scales,
+                                                                       float *__restrict__ rstd_out, int64_t rows,
+                                                                       int64_t cols, int nblk)
+{
+    constexpr int kThreads = TPR == 64 ? kBlock : TPR, kRows = kThreads / TPR;
+    __shared__ float part[2][kThreads / 64];
+    typedef typename pv_vec8<T>::raw raw;
+    const int t = threadIdx.x % TPR, units = nblk * 4;
+    int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
+    const int64_t stride = (int64_t)gridDim.x * kRows;
+    raw a[NV], b[NV];
+    auto load = [&](int64_t at) {
 #pragma unroll
-    for (int u = 0; u < NV; ++u) {
-        const int unit = u * TPR + t, valid = (int)cols - unit * 8;
-        if (residual) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[u][i] = (float)(T)(v[u][i] + r[u][i]);
+        for (int u = 0; u < NV; ++u) {
+            const int unit = u * TPR + t, valid = (int)cols - unit * 8;
+            a[u] = pv_load8_raw(x + at * cols + (int64_t)unit * 8, valid);
+            if (residual) b[u] = pv_load8_raw(residual + at * cols + (int64_t)unit * 8, valid);
         }
-        if (h) pv_store8(h + base + (int64_t)unit * 8, valid, v[u]);
+    };
+    if (row < rows) load(row);
+    float w[NV][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(v[u][i], v[u][i], sum);
-    }
-    sum = pv_block_reduce<TPR>(sum, part, pv_add{});
-    const float rstd = 1.0f / sqrtf(sum / (float)cols + eps);
-    if (rstd_out && t == 0) rstd_out[row] = rstd;
-    if (!y && !codes) return;
+    for (int u = 0; u < NV; ++u) pv_load8(weight + (u * TPR + t) * 8, (int)cols - (u * TPR + t) * 8, w[u]);
+    for (int turn = 0; row < rows; row += stride, turn ^= 1) {      // a whole wave's row, and a whole block's where it meets in barriers
+        float v[NV][8], sum = 0.0f;
 #pragma unroll
-    for (int u = 0; u < NV; ++u) {
-        const int unit = u * TPR + t, valid = (int)cols - unit * 8;
-        float w[8];
-        pv_load8(weight + (int64_t)unit * 8, valid, w);
+        for (int u = 0; u < NV; ++u) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[u][i] = (v[u][i] * rstd) * w[i];
-        if (y) pv_store8(y + base + (int64_t)unit * 8, valid, v[u]);
-        if (codes && unit < units) {
-            const unsigned scale = pv_mx_scale<FMT>(pv_mx_largest(v[u]));
-            const pv_u2 c = pv_mx_encode<FMT>(v[u], scale);
-            const int64_t at = row * units + unit;
-            if constexpr (FMT == PV_MX_E2M1) reinterpret_cast<unsigned *>(codes)[at] = c.x;
-            else reinterpret_cast<pv_u2 *>(codes)[at] = c;
-            if ((unit & 3) == 0) scales[at >> 2] = (uint8_t)scale;
+            for (int i = 0; i < 8; ++i) {
+                v[u][i] = (float)a[u][i];
+                if (residual) v[u][i] = (float)(T)(v[u][i] + (float)b[u][i]);
+                sum = fmaf(v[u][i], v[u][i], sum);
+            }
         }
+        if (row + stride < rows) load(row + stride);                // (another row: the outputs may lie on the inputs)
+#pragma unroll
+        for (int u = 0; u < NV; ++u)
+            if (h) pv_store8(h + row * cols + (u * TPR + t) * 8, (int)cols - (u * TPR + t) * 8, v[u]);
+        sum = pv_block_reduce<TPR>(sum, part[turn], pv_add{});
+        const float rstd = 1.0f / sqrtf(sum / (float)cols + eps);
+        if (rstd_out && t == 0) rstd_out[row] = rstd;
+#pragma unroll
+        for (int u = 0; u < NV; ++u)
+            norm_out<T, FMT>(v[u], rstd, w[u], (int)cols - (u * TPR + t) * 8, u * TPR + t, units, row, cols, y, codes, scales);
     }
 }
 
@@ -101,22 +118,14 @@ __global__ __launch_bounds__(1024) void k_rms_norm_long(const T *x, const T *res
         load(unit, valid, v);
         if (h) pv_store8(h + base + (int64_t)unit * 8, valid, v);
         pv_load8(weight + (int64_t)unit * 8, valid, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (v[i] * rstd) * w[i];
-        if (y) pv_store8(y + base + (int64_t)unit * 8, valid, v);
-        if (codes) {
-            const unsigned scale = pv_mx_scale<FMT>(pv_mx_largest(v));
-            const pv_u2 c = pv_mx_encode<FMT>(v, scale);
-            const int64_t at = row * units + unit;
-            if constexpr (FMT == PV_MX_E2M1) reinterpret_cast<unsigned *>(codes)[at] = c.x;
-            else reinterpret_cast<pv_u2 *>(codes)[at] = c;
-            if ((unit & 3) == 0) scales[at >> 2] = (uint8_t)scale;
-        }
+        norm_out<T, FMT>(v, rstd, w, valid, unit, units, row, cols, y, codes, scales);
     }
 }
 
-// Backward: block b takes the rows b, b + gridDim.x, ... and keeps its sums for dweight in registers from row to row;
-// they leave once, as one row of `partial`.
+// Backward: block b takes the rows b, b + gridDim.x, ... with the weights and its sums for dweight in registers from row to
+// row; the sums leave once, as one row of `partial`.  A row stays as it was read, and the factors are formed twice, which takes
+// half the registers.  Where they leave room for one block a compute unit only and for another row (kAhead), that row is on its
+// way while this one is reduced.
 template <class T, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS) void k_rms_norm_backward(const T *dy, const T *dh, const T *h,
                                                                const float *__restrict__ weight,
@@ -124,60 +133,66 @@ __global__ __launch_bounds__(THREADS) void k_rms_norm_backward(const T *dy, cons
                                                                float *__restrict__ partial, int64_t rows, int64_t cols)
 {
     __shared__ float part[2][THREADS / 64];
+    typedef typename pv_vec8<T>::raw raw;
     const int t = threadIdx.x;
-    float acc[NV][8];
+    float acc[NV][8], w[NV][8];
 #pragma unroll
-    for (int u = 0; u < NV; ++u)
+    for (int u = 0; u < NV; ++u) {
+        pv_load8(weight + (u * THREADS + t) * 8, (int)cols - (u * THREADS + t) * 8, w[u]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[u][i] = 0.0f;
+    }
+    constexpr bool kAhead = NV == 3 && sizeof(T) == 2;
+    raw next[kAhead ? 3 * NV : 1];
+    auto load = [&](int64_t row, raw *a, raw *b, raw *c) {
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+            const int first = (u * THREADS + t) * 8, valid = (int)cols - first;
+            a[u] = pv_load8_raw(dy + row * cols + first, valid);
+            b[u] = pv_load8_raw(h + row * cols + first, valid);
+            if (dh && dx) c[u] = pv_load8_raw(dh + row * cols + first, valid);
+        }
+    };
+    if constexpr (kAhead) load(blockIdx.x, next, next + NV, next + 2 * NV);
     int turn = 0;
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 1) {
-        const int64_t base = row * cols;
         const float rstd = rstd_in[row];
-        float g[NV][8], n[NV][8];
+        raw a[NV], b[NV], c[NV];
+        if constexpr (kAhead) {
+#pragma unroll
+            for (int u = 0; u < NV; ++u) a[u] = next[u], b[u] = next[NV + u], c[u] = next[2 * NV + u];
+            if (row + gridDim.x < rows) load(row + gridDim.x, next, next + NV, next + 2 * NV);      // (another row: dx may lie on an input)
+        } else {
+            load(row, a, b, c);
+        }
         float dot = 0.0f;
 #pragma unroll
-        for (int u = 0; u < NV; ++u) {
-            const int64_t at = (int64_t)(u * THREADS + t) * 8;
-            const int valid = (int)cols - (u * THREADS + t) * 8;
-            pv_load8(dy + base + at, valid, g[u]);
-            pv_load8(h + base + at, valid, n[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < NV; ++u) {
-            const int64_t at = (int64_t)(u * THREADS + t) * 8;
-            const int valid = (int)cols - (u * THREADS + t) * 8;
-            float w[8];
-            pv_load8(weight + at, valid, w);
+        for (int u = 0; u < NV; ++u)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                n[u][i] *= rstd;
-                acc[u][i] = fmaf(g[u][i], n[u][i], acc[u][i]);
-                g[u][i] *= w[i];
-                dot = fmaf(g[u][i], n[u][i], dot);
+                const float n = (float)b[u][i] * rstd;
+                acc[u][i] = fmaf((float)a[u][i], n, acc[u][i]);
+                dot = fmaf((float)a[u][i] * w[u][i], n, dot);
             }
-        }
         if (!dx) continue;
         const float mean = pv_block_reduce<THREADS>(dot, part[turn], pv_add{}) / (float)cols;
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
-            const int64_t at = (int64_t)(u * THREADS + t) * 8;
-            const int valid = (int)cols - (u * THREADS + t) * 8;
+            const int first = (u * THREADS + t) * 8;
             float d[8];
-            if (dh) pv_load8(dh + base + at, valid, d);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float e = rstd * fmaf(-n[u][i], mean, g[u][i]);
-                d[i] = dh ? d[i] + e : e;
+                const float e = rstd * fmaf(-((float)b[u][i] * rstd), mean, (float)a[u][i] * w[u][i]);
+                d[i] = dh ? (float)c[u][i] + e : e;
             }
-            pv_store8(dx + base + at, valid, d);
+            pv_store8(dx + row * cols + first, (int)cols - first, d);
         }
     }
     if (!partial) return;
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-        const int64_t at = (int64_t)(u * THREADS + t) * 8;
-        pv_store8(partial + (int64_t)blockIdx.x * cols + at, (int)cols - (int)at, acc[u]);
+        const int first = (u * THREADS + t) * 8;
+        pv_store8(partial + (int64_t)blockIdx.x * cols + first, (int)cols - first, acc[u]);
     }
 }
 
@@ -252,15 +267,22 @@ __global__ __launch_bounds__(kBlock) void k_sum_partials(const float *__restrict
     }
 }
 
-// f(integral_constant<int, NV>) for the smallest of 1, 2, 4, 8 that covers `units` with `threads`
-template <class F>
+constexpr int kMostUnits = 2048;      // of eight values, of a row in registers
+
+// f(integral_constant<int, NV>), NV = ceil(units / threads) <= MAX_NV
+template <int MAX_NV, class F>
 pv_status for_nv(int units, int threads, F f)
 {
-    const int nv = (units + threads - 1) / threads;
-    if (nv <= 1) return f(std::integral_constant<int, 1>{});
-    if (nv <= 2) return f(std::integral_constant<int, 2>{});
-    if (nv <= 4) return f(std::integral_constant<int, 4>{});
-    return f(std::integral_constant<int, 8>{});
+    if (units <= threads) return f(std::integral_constant<int, 1>{});
+    if constexpr (MAX_NV > 2) {
+        if (units > 2 * threads) {
+            if constexpr (MAX_NV > 3) {
+                if (units > 3 * threads) return f(std::integral_constant<int, 4>{});
+            }
+            return f(std::integral_constant<int, 3>{});
+        }
+    }
+    return f(std::integral_constant<int, 2>{});
 }
 
 }  // namespace
@@ -280,22 +302,28 @@ pv_status pv_launch_rms_norm(pv_ctx *ctx, int64_t rows, int64_t cols, int type, 
             PV_HIP(ctx, hipGetLastError());
             return PV_OK;
         };
-        if (units > kBlock * 8) {
+        if (units > kMostUnits) {
             const auto k = format == PV_MX_E2M1 ? k_rms_norm_long<T, PV_MX_E2M1> : k_rms_norm_long<T, PV_MX_E4M3>;
             return launch(k, (unsigned)rows, 1024);
         }
-        // a wave a row where that fills the chip and its registers hold it
-        if (units <= 64 * 8 && rows >= 1024)
-            return for_nv(units, 64, [&](auto nv) {
+        // short rows, enough of them to fill the chip: a wave a row
+        if (units <= 128 && rows >= 1024) {
+            const unsigned blocks = (unsigned)((rows + 3) / 4);
+            auto wave = [&](auto nv) {
                 constexpr int NV = decltype(nv)::value;
-                const auto k = format == PV_MX_E2M1 ? k_rms_norm<T, 64, NV, PV_MX_E2M1> : k_rms_norm<T, 64, NV, PV_MX_E4M3>;
-                return launch(k, (unsigned)((rows + 3) / 4), kBlock);
-            });
-        return for_nv(units, kBlock, [&](auto nv) {
-            constexpr int NV = decltype(nv)::value;
-            const auto k = format == PV_MX_E2M1 ? k_rms_norm<T, kBlock, NV, PV_MX_E2M1> : k_rms_norm<T, kBlock, NV, PV_MX_E4M3>;
-            return launch(k, (unsigned)rows, kBlock);
-        });
+                return launch(format == PV_MX_E2M1 ? k_rms_norm<T, 64, NV, PV_MX_E2M1> : k_rms_norm<T, 64, NV, PV_MX_E4M3>,
+                              blocks < 4096 ? blocks : 4096, kBlock);
+            };
+            return units <= 64 ? wave(std::integral_constant<int, 1>{}) : wave(std::integral_constant<int, 2>{});
+        }
+        auto block = [&](auto threads, auto nv) {
+            constexpr int THREADS = decltype(threads)::value, NV = decltype(nv)::value;
+            const int64_t most = 256 * (2048 / THREADS);      // as many threads as the chip holds
+            return launch(format == PV_MX_E2M1 ? k_rms_norm<T, THREADS, NV, PV_MX_E2M1> : k_rms_norm<T, THREADS, NV, PV_MX_E4M3>,
+                          (unsigned)(rows < most ? rows : most), THREADS);
+        };
+        if (units <= 1024) return for_nv<4>(units, 256, [&](auto nv) { return block(std::integral_constant<int, 256>{}, nv); });
+        return for_nv<4>(units, 512, [&](auto nv) { return block(std::integral_constant<int, 512>{}, nv); });
     });
 }
 
@@ -303,9 +331,10 @@ pv_status pv_launch_rms_norm_backward(pv_ctx *ctx, int64_t rows, int64_t cols, i
                                       const void *dh, const void *h, const float *weight, const float *rstd,
                                       void *dx, float *dweight)
 {
-    constexpr int kThreads = 512;
-    constexpr int64_t kMaxBlocks = 512;      // two a compute unit
-    const int64_t blocks = rows < kMaxBlocks ? rows : kMaxBlocks;
+    const int units = (int)((cols + 7) / 8);
+    // each block leaves a row of sums that is written and read: no more of them than an eighth of the rows is worth
+    const int64_t most = units > 1024 ? 256 : rows >= 4096 ? 1024 : 512;
+    const int64_t blocks = rows < most ? rows : most;
     float *partial = nullptr;
     if (dweight && blocks > 1) {
         void *p;
@@ -316,7 +345,6 @@ pv_status pv_launch_rms_norm_backward(pv_ctx *ctx, int64_t rows, int64_t cols, i
         partial = dweight;
     }
     pv_timed t(ctx, PV_K_RMS_NORM);
-    const int units = (int)((cols + 7) / 8);
     pv_status st = pv_for_dtype(type, [&](auto v) {
         using T = decltype(v);
         auto launch = [&](auto k, int threads) {
@@ -326,11 +354,9 @@ pv_status pv_launch_rms_norm_backward(pv_ctx *ctx, int64_t rows, int64_t cols, i
             PV_HIP(ctx, hipGetLastError());
             return PV_OK;
         };
-        if (units > kThreads * 4) return launch(k_rms_norm_backward_long<T>, 1024);
-        return for_nv(units, kThreads, [&](auto nv) {
-            constexpr int NV = decltype(nv)::value < 4 ? decltype(nv)::value : 4;
-            return launch(k_rms_norm_backward<T, kThreads, NV>, kThreads);
-        });
+        if (units > kMostUnits) return launch(k_rms_norm_backward_long<T>, 1024);
+        if (units <= 256) return launch(k_rms_norm_backward<T, 256, 1>, 256);
+        return for_nv<4>(units, 512, [&](auto nv) { return launch(k_rms_norm_backward<T, 512, decltype(nv)::value>, 512); });
     });
     if (st != PV_OK || partial == dweight) return st;
     hipLaunchKernelGGL(k_sum_partials, dim3((unsigned)((cols + 31) / 32)), dim3(kBlock), 0, ctx->stream, partial,

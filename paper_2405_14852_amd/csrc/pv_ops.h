@@ -69,6 +69,17 @@ __device__ __forceinline__ void pv_load8(const T *p, int valid, float (&v)[8])
     }
 }
 
+// the same, not yet converted
+template <class T>
+__device__ __forceinline__ typename pv_vec8<T>::raw pv_load8_raw(const T *p, int valid)
+{
+    if (valid >= 8) return *reinterpret_cast<const typename pv_vec8<T>::type *>(p);
+    typename pv_vec8<T>::raw r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = i < valid ? p[i] : (T)0.0f;
+    return r;
+}
+
 template <class T>
 __device__ __forceinline__ void pv_store8(T *p, int valid, const float (&v)[8])
 {

@@ -96,16 +96,20 @@ def distill(logits, ids, top, t, weight=None):
     at = torch.where(there, ids, 0)
     u = torch.where(there, u, -math.inf)
     any_ = (u > -math.inf).any(1) if ids.shape[1] else torch.zeros(R, dtype=torch.bool)
-    lse = torch.logsumexp(z, 1)
+    # the largest logit first: a row of -3e38 leaves no digit of the sum's logarithm otherwise, in 64 bits neither
+    largest = z.amax(1, keepdim=True)
+    z = z - largest
+    log_sum = torch.log(torch.exp(z).sum(1))
+    lse = largest[:, 0] + log_sum
     if ids.shape[1]:
         log_p = torch.where(any_[:, None], u - torch.logsumexp(u, 1, keepdim=True), -math.inf)
     else:
         log_p = u
     p = torch.exp(log_p)
-    log_q = z.gather(1, at) - lse[:, None]
+    log_q = z.gather(1, at) - log_sum[:, None]
     kl = torch.where(p > 0, p * (log_p - log_q), 0.0).sum(1)
     target = torch.zeros(R, V, dtype=torch.float64).scatter_add(1, at, torch.where(there, p, 0.0))
-    grad = t * (torch.exp(z - lse[:, None]) - target)
+    grad = t * (torch.exp(z - log_sum[:, None]) - target)
     on = (w != 0) & any_
     loss = torch.where(on, w * t * t * kl, 0.0)
     grad = torch.where(on[:, None], w[:, None] * grad, 0.0)
