@@ -501,40 +501,86 @@ __global__ __launch_bounds__(256) void k_pad_scales(const uint8_t *__restrict__ 
 // ---------------------------------------------------------------- operands of the gradients
 
 // A matrix [rows, cols] (codes, or bf16) as bf16, transposed: out [cols, pitch] with pitch >= rows, zeros behind `rows`.
-// Tiles of 64 x 64 through LDS, padded by a bank.
+struct turned {
+    const uint8_t *codes, *scales;
+    pv_bf16 *out;
+    int64_t rows, cols, pitch;
+    int kind, nblk;
+    unsigned ctiles, blocks;
+};
+
+// 16 consecutive values of a row as eight words of bf16 pairs; zeros outside the matrix
 template <int KIND>
-__global__ __launch_bounds__(256) void k_transpose(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
-                                                   int64_t rows, int64_t cols, int nblk, pv_bf16 *__restrict__ out,
-                                                   int64_t pitch, int ctiles)
+__device__ __forceinline__ void load_pairs(const turned &m, int64_t row, int64_t col, unsigned (&v)[8])
 {
-    __shared__ pv_bf16 tile[64][66];
-    const int64_t r0 = (int64_t)(blockIdx.x / ctiles) * 64, c0 = (int64_t)(blockIdx.x % ctiles) * 64;
-    for (int u = threadIdx.x; u < 512; u += 256) {
-        const int r = u >> 3, c = (u & 7) * 8;
-        const int64_t row = r0 + r, col = c0 + c;
-        float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-        if (row < rows) {
-            if constexpr (KIND == kBF16) {
-                pv_load8(reinterpret_cast<const pv_bf16 *>(codes) + row * cols + col, (int)min(cols - col, (int64_t)8), v);
-            } else if (col < (int64_t)nblk * 32) {
-                const int64_t at = row * nblk * 4 + col / 8;
-                pv_u2 e = {0u, 0u};
-                if constexpr (KIND == kE2M1) e.x = reinterpret_cast<const unsigned *>(codes)[at];
-                else e = reinterpret_cast<const pv_u2 *>(codes)[at];
-                pv_mx_decode<KIND == kBF16 ? 0 : KIND>(e, pv_mx_power(scales[at >> 2]), v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0u;
+    if (row >= m.rows) return;
+    if constexpr (KIND == kBF16) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int64_t at = col + 8 * half;
+            const b8v r = pv_load8_raw(reinterpret_cast<const pv_bf16 *>(m.codes) + row * m.cols + at, (int)max(min(m.cols - at, (int64_t)8), (int64_t)0));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[4 * half + i] = __builtin_bit_cast(pv_u4, r)[i];
+        }
+    } else {
+        if (col >= (int64_t)m.nblk * kMxBlock) return;
+        const float power = pv_mx_power(m.scales[row * m.nblk + col / kMxBlock]);
+        const int64_t at = row * m.nblk * (KIND == kE2M1 ? 16 : 32) + (KIND == kE2M1 ? col / 2 : col);
+        if constexpr (KIND == kE2M1) {
+            const pv_u2 c = *reinterpret_cast<const pv_u2 *>(m.codes + at);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                v[4 * i + 0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], power, 0));
+                v[4 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], power, 1));
+                v[4 * i + 2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], power, 2));
+                v[4 * i + 3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], power, 3));
+            }
+        } else {
+            const pv_u4 c = *reinterpret_cast<const pv_u4 *>(m.codes + at);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i + 0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[i], power, false));
+                v[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[i], power, true));
             }
         }
+    }
+}
+
+// Up to three matrices in one launch, in tiles of 64 x 64 through LDS.  Rows there are 33 words apart: the 64 lanes that read a
+// word each - 8 pairs of columns of 8 rows 8 apart - meet 64 banks.  Bound by the bytes, most of them written.
+__global__ __launch_bounds__(256) void k_transpose(turned m0, turned m1, turned m2)
+{
+    __shared__ unsigned tile[64][33];
+    unsigned b = blockIdx.x;
+    const bool first = b < m0.blocks, second = !first && b - m0.blocks < m1.blocks;
+    const turned m = first ? m0 : second ? m1 : m2;
+    b -= first ? 0 : second ? m0.blocks : m0.blocks + m1.blocks;
+    const int64_t r0 = (int64_t)(b / m.ctiles) * 64, c0 = (int64_t)(b % m.ctiles) * 64;
+    {
+        const int r = threadIdx.x >> 2, c = (threadIdx.x & 3) * 16;
+        unsigned v[8];
+        if (m.kind == kE2M1) load_pairs<kE2M1>(m, r0 + r, c0 + c, v);
+        else if (m.kind == kE4M3) load_pairs<kE4M3>(m, r0 + r, c0 + c, v);
+        else load_pairs<kBF16>(m, r0 + r, c0 + c, v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) tile[r][c + i] = (pv_bf16)v[i];
+        for (int i = 0; i < 8; ++i) tile[r][c / 2 + i] = v[i];
     }
     __syncthreads();
-    for (int u = threadIdx.x; u < 512; u += 256) {
-        const int c = u >> 3, r = (u & 7) * 8;
-        if (c0 + c >= cols || r0 + r >= pitch) continue;       // the pitch is a multiple of 8
-        b8v v;
+    const int c = threadIdx.x >> 3, r = (threadIdx.x & 7) * 8;
+    unsigned v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = tile[r + i][c];
-        *reinterpret_cast<b8v *>(out + (c0 + c) * pitch + r0 + r) = v;
+    for (int i = 0; i < 8; ++i) v[i] = tile[r + i][c];
+    if (r0 + r >= m.pitch) return;                     // (a multiple of 8)
+#pragma unroll
+    for (int odd = 0; odd < 2; ++odd) {
+        const int64_t col = c0 + 2 * c + odd;
+        if (col >= m.cols) return;
+        pv_u4 o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_perm(v[2 * i + 1], v[2 * i], odd ? 0x07060302u : 0x05040100u);
+        *reinterpret_cast<pv_u4 *>(m.out + col * m.pitch + r0 + r) = o;
     }
 }
 
@@ -643,13 +689,20 @@ int64_t padded(int64_t n) { return pv_mx_blocks(n) * kMxBlock; }
 
 size_t round16(size_t bytes) { return (bytes + 15) & ~(size_t)15; }
 
-pv_status transpose(pv_ctx *ctx, int kind, const void *codes, const uint8_t *scales, int64_t rows, int64_t cols, pv_bf16 *out)
+turned turn(int kind, const void *codes, const uint8_t *scales, int64_t rows, int64_t cols, pv_bf16 *out)
 {
     const int64_t pitch = padded(rows), ctiles = (cols + 63) / 64, blocks = ctiles * ((pitch + 63) / 64);
+    // (a side is below 2^31, and products of 2^25 tiles either way do not fit memory: what is too large shows as 2^31)
+    return {static_cast<const uint8_t *>(codes), scales, out, rows, cols, pitch, kind, (int)pv_mx_blocks(cols), (unsigned)ctiles,
+            (unsigned)(blocks < ((int64_t)1 << 31) ? blocks : (int64_t)1 << 31)};
+}
+
+pv_status transpose(pv_ctx *ctx, const turned *m, int n)
+{
+    const turned none = {};
+    const int64_t blocks = (int64_t)m[0].blocks + (n > 1 ? m[1].blocks : 0) + (n > 2 ? m[2].blocks : 0);
     if (blocks >= (int64_t)1 << 31) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many tiles of the gradients' operands");
-    const auto k = kind == kE2M1 ? k_transpose<kE2M1> : kind == kE4M3 ? k_transpose<kE4M3> : k_transpose<kBF16>;
-    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, static_cast<const uint8_t *>(codes), scales, rows,
-                       cols, (int)pv_mx_blocks(cols), out, pitch, (int)ctiles);
+    hipLaunchKernelGGL(k_transpose, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, m[0], n > 1 ? m[1] : none, n > 2 ? m[2] : none);
     PV_HIP(ctx, hipGetLastError());
     return PV_OK;
 }
@@ -739,8 +792,13 @@ pv_status pv_launch_mx_product_grads(pv_ctx *ctx, int64_t tokens, int64_t out, i
     float *partial = static_cast<float *>(p);
     pv_bf16 *WT = reinterpret_cast<pv_bf16 *>(static_cast<uint8_t *>(p) + sums), *DYP = WT + wt, *XT = DYP + dyp, *DYT = XT + xt;
     pv_timed t(ctx, PV_K_MX_PRODUCT);
+    turned m[3];
+    int n = 0;
+    if (dX) m[n++] = turn(kE2M1, w_codes, w_scales, out, in, WT);
+    if (dW) m[n++] = turn(x_format, x_codes, x_scales, tokens, in, XT);
+    if (dW) m[n++] = turn(kBF16, dY, nullptr, tokens, out, DYT);
+    if ((st = transpose(ctx, m, n)) != PV_OK) return st;
     if (dX) {
-        if ((st = transpose(ctx, kE2M1, w_codes, w_scales, out, in, WT)) != PV_OK) return st;
         if (pad) {
             const int64_t blocks = (tokens * (op / 8) + 255) / 256;
             if (blocks >= (int64_t)1 << 31) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many rows of dY");
@@ -756,8 +814,6 @@ pv_status pv_launch_mx_product_grads(pv_ctx *ctx, int64_t tokens, int64_t out, i
         if (st != PV_OK) return st;
     }
     if (dW) {
-        if ((st = transpose(ctx, x_format, x_codes, x_scales, tokens, in, XT)) != PV_OK) return st;
-        if ((st = transpose(ctx, kBF16, dY, nullptr, tokens, out, DYT)) != PV_OK) return st;
         st = launch<kBF16, kBF16>(ctx, cw, plain(XT, in, tp), plain(DYT, out, tp), (int)(tp / 32), 0, partial, dW);
     }
     return st;
