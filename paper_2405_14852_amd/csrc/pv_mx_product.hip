@@ -266,10 +266,9 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tiled(operand w, operan
     constexpr int kScales = WK == kBF16 ? 0 : (BM + BN) * 16;
     constexpr int kStage = kWBytes + kXBytes;
     constexpr int kWLoads = kWBytes / 1024 / kWaves, kXLoads = kXBytes / 1024 / kWaves, kData = kWLoads + kXLoads;
-    constexpr int kSLoads = WK == kBF16 ? 0 : (BM + BN) / 64 / kWaves;
+    constexpr int kSLoads = WK == kBF16 ? 0 : (BM + BN + 64 * kWaves - 1) / 64 / kWaves;
     constexpr int kSlices = step_of<WK>::slices;
     static_assert(kWLoads * 1024 * kWaves == kWBytes && kXLoads * 1024 * kWaves == kXBytes, "whole loads a wave");
-    static_assert(WK == kBF16 || kSLoads * 64 * kWaves == BM + BN, "whole loads of scales a wave");
     static_assert(BM % 16 == 0 && FM * 32 * WM == BM && FN * 32 * WN == BN && kSlices % 2 == 0 && NS >= 2, "tile");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[NS * kStage + 2 * kScales];
 
@@ -333,6 +332,7 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tiled(operand w, operan
 #pragma unroll
         for (int i = 0; i < kSLoads; ++i) {
             const int first = ((quarter * kSLoads + i) * kWaves + wave) * 16;
+            if (first >= BM + BN) continue;
             const bool of_w = first < BM;
             const int row = min((of_w ? first : first - BM) + (lane >> 2), of_w ? wlast : xlast);
             fetch<4>((of_w ? wscale : xscale) + ((unsigned)row * (unsigned)p.scale_pitch + at), base + NS * kStage + (group & 1) * kScales + first * 16);
@@ -598,36 +598,41 @@ __global__ __launch_bounds__(256) void k_pad_rows(const pv_bf16 *__restrict__ in
 
 // ---------------------------------------------------------------- which kernel
 
-constexpr int kDirect = 0, kSmallTile = 1, kLargeTile = 2;
+// tiles of W's rows by X's: 128 x 64, 128 x 128 (both two blocks a compute unit) and 256 x 256 (one)
+constexpr int kNarrow = 0, kMiddle = 1, kLarge = 2, kDirect = 3;
 
 struct choice {
     int tile, splits;
     size_t partial;          // bytes of the splits' sums
 };
 
-// The variant that is expected to take least, from what the parts take (us): a step of a large tile on each of 256 compute units, of
-// two small tiles on each, or of one; a launch's start and end; another launch that adds the splits' sums, which are
-// written and read.  Measured on 4096 in -> 4096 out, e4m3, bf16 out (small tiles with 1, 2, 4, 8 splits | large ones with 1, 2, 4):
-//   128 tokens 18.0 16.2 15.8 19.6 | 41.6 29.4 23.6      512 tokens 19.5 21.6 25.8 35.3 | 43.8 37.0 30.9
-//   2048 tokens 37.2 60.5 81.2 133 | 47.9 52.0 72.3      131 tokens of 14336, both e2m1: 40.5 27.2 20.8 24.3 | 90.4 53.7 35.1
-// Up to 16 tokens W is read straight to registers, at any size: 16 rows of X fill one instruction (32 tokens, 4096 -> 11008:
-// 28.5 us that way, 14.7 through tiles).
+// The variant that is expected to take least, from what the parts take: a step of one block or of two on a compute unit, in parts of
+// a large tile's step (us); a launch's start and end; another launch that adds the splits' sums, which are written and read.
+// Measured (us), 4096 -> 4096, e4m3, bf16 out, narrow | middle | large tiles, with 1, 2, 4 splits:
+//   64 tokens 13.7 12.4 11.6 | 19.9 15.2 12.9 | 41.3 26.9 19.9        128 tokens 14.1 13.5 14.0 | 20.1 17.0 15.8 | 41.6 29.4 23.6
+//   300 tokens 14.5 19.7 21.5 | 19.9 20.2 23.1         without splits: 512 tokens 16.2 | 21.2 | 45.9, 1024 tokens 24.1 | 23.9 | 47.3,
+//   2048 tokens 45.0 | 36.1 | 50.9, 3000 tokens 62.2 | 51.6 | 53.0, 4096 tokens 81.2 | 65.5 | 57.1
+//   131 tokens 14336 -> 4096, both e2m1, f32 out, with 1, 2, 4, 8: 36.2 24.0 22.3 23.4 | 45.6 29.4 21.6 24.6
+// Up to 16 tokens W is read straight to registers, at any size (32 tokens, 4096 -> 11008: 28.5 that way, 12.8 through tiles).
 template <int WK, int XK>
 choice choose(int64_t out, int64_t tokens, int nblk)
 {
+    constexpr struct {
+        int bm, bn, at_once;
+        double one, two;
+    } kTiles[] = {{128, 64, 512, 0.175, 0.375}, {128, 128, 512, WK == kBF16 ? 0.4 : 0.28, 0.6}, {256, 256, 256, 1.0, 1.0}};
     constexpr double kStep = WK == kBF16 ? 1.5 : XK == kE4M3 ? 1.6 : 1.15;
-    constexpr double kTwoSmall = 0.6 * kStep, kOneSmall = (WK == kBF16 ? 0.4 : 0.3) * kStep;
     const int steps = (nblk + step_of<WK>::blocks - 1) / step_of<WK>::blocks;
-    choice best = {kLargeTile, 1, 0};
+    choice best = {kLarge, 1, 0};
     double least = 1e300;
-    for (int tile = kSmallTile; tile <= kLargeTile; ++tile) {
-        const int side = tile == kLargeTile ? 256 : 128, at_once = tile == kLargeTile ? 256 : 512;
-        const int64_t tiles = ((out + side - 1) / side) * ((tokens + side - 1) / side);
+    for (int tile = kNarrow; tile <= kLarge; ++tile) {
+        const auto &t = kTiles[tile];
+        const int64_t tiles = ((out + t.bm - 1) / t.bm) * ((tokens + t.bn - 1) / t.bn);
         for (int splits = 1; splits <= 16 && splits * 4 <= (steps > 4 ? steps : 4); splits *= 2) {
-            const int64_t blocks = tiles * splits, rounds = blocks / at_once, rest = blocks % at_once;
-            const double mine = (steps + splits - 1) / splits, full = tile == kLargeTile ? kStep : kTwoSmall;
-            double us = (double)rounds * (mine * full + 4.0);
-            if (rest) us += mine * (tile == kSmallTile && rest <= 256 ? kOneSmall : full) + 4.0;
+            const int64_t blocks = tiles * splits, rounds = blocks / t.at_once, rest = blocks % t.at_once;
+            const double mine = (double)((steps + splits - 1) / splits) * kStep;
+            double us = (double)rounds * (mine * t.two + 4.0);
+            if (rest) us += mine * (rest <= 256 ? t.one : t.two) + 4.0;
             if (splits > 1) us += 4.0 + (double)splits * (double)(out * tokens) * 8 / 4e6;
             if (us < least) least = us, best = {tile, splits, splits > 1 ? (size_t)(splits * out * tokens) * 4 : 0};
         }
@@ -673,7 +678,8 @@ pv_status launch(pv_ctx *ctx, const choice &c, const operand &w, const operand &
 {
     const tiling p = {nblk, 0, 0, c.splits, scale_pitch, partial};
     constexpr int NS = WK == kBF16 ? 2 : 3;
-    if (c.tile == kSmallTile) return launch_tiled<WK, XK, 128, 128, 2, 2, NS>(ctx, w, x, p, Y);
+    if (c.tile == kNarrow) return launch_tiled<WK, XK, 128, 64, 2, 2, NS>(ctx, w, x, p, Y);
+    if (c.tile == kMiddle) return launch_tiled<WK, XK, 128, 128, 2, 2, NS>(ctx, w, x, p, Y);
     return launch_tiled<WK, XK, 256, 256, 2, 4, NS>(ctx, w, x, p, Y);
 }
 

@@ -148,7 +148,7 @@ def test_product(ctx, tokens, out, inn, fmt, dtype):
 
 
 @pytest.mark.parametrize("fmt,dtype", [("e4m3", torch.bfloat16), ("e2m1", torch.float32), ("e4m3", torch.float32)], ids=str)
-@pytest.mark.parametrize("tokens,out,inn", [(2100, 4203, 300), (4097, 2049, 1024)])
+@pytest.mark.parametrize("tokens,out,inn", [(1100, 4203, 300), (2100, 4203, 300), (4097, 2049, 1024)])
 def test_product_in_large_tiles(ctx, tokens, out, inn, fmt, dtype):
     test_product(ctx, tokens, out, inn, fmt, dtype)
 
@@ -183,7 +183,7 @@ def test_product_of_scales_far_apart(ctx, fmt, dtype, scale):
 @pytest.mark.parametrize("fmt", ["e2m1", "e4m3"])
 @pytest.mark.parametrize("tokens,out,inn", [(1, 1, 1), (2, 32, 32), (5, 33, 70), (64, 64, 64), (33, 130, 96), (100, 257, 300),
                                             (256, 256, 512), (300, 200, 520), (129, 512, 384), (40, 4100, 70), (4100, 40, 70),
-                                            (70, 4203, 2100)])
+                                            (70, 4203, 2100), (2100, 96, 2101)])
 def test_product_grads(ctx, tokens, out, inn, fmt, dx_type):
     xc, xs, wc, ws = operands(tokens, out, inn, fmt, seed=tokens * 3 + out + inn)
     dy = torch.randn(tokens, out, generator=gen(9)).to(torch.bfloat16)
