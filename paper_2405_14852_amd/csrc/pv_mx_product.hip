@@ -643,8 +643,6 @@ choice choose(int64_t out, int64_t tokens, int nblk)
 template <int WK, int XK, int BM, int BN, int WM, int WN, int NS, class T>
 pv_status launch_tiled(pv_ctx *ctx, const operand &w, const operand &x, tiling p, T *Y)
 {
-    // a tile's rows lie within 32 bits of its first
-    if (w.pitch >= 1 << 24 || x.pitch >= 1 << 24) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "more than 16 MiB a row of an operand");
     p.wtiles = (w.rows + BM - 1) / BM;
     p.xtiles = (x.rows + BN - 1) / BN;
     const int64_t blocks = (int64_t)p.wtiles * p.xtiles * p.splits;
@@ -677,8 +675,11 @@ template <int WK, int XK, class T>
 pv_status launch(pv_ctx *ctx, const choice &c, const operand &w, const operand &x, int nblk, int64_t scale_pitch, float *partial, T *Y)
 {
     const tiling p = {nblk, 0, 0, c.splits, scale_pitch, partial};
+    // Stages: as many as LDS holds for two blocks of the smaller tiles or one of the large, but no more than three.  (bf16, narrow,
+    // gradients of 256 x 2048 x 1024: two 23.2 us, three 20.3; codes with four or five stages take what they take with three:
+    // what the smaller tiles wait for is the rate of the L2, 15 TB/s of the 256 compute units together.)
     constexpr int NS = WK == kBF16 ? 2 : 3;
-    if (c.tile == kNarrow) return launch_tiled<WK, XK, 128, 64, 2, 2, NS>(ctx, w, x, p, Y);
+    if (c.tile == kNarrow) return launch_tiled<WK, XK, 128, 64, 2, 2, 3>(ctx, w, x, p, Y);
     if (c.tile == kMiddle) return launch_tiled<WK, XK, 128, 128, 2, 2, NS>(ctx, w, x, p, Y);
     return launch_tiled<WK, XK, 256, 256, 2, 4, NS>(ctx, w, x, p, Y);
 }
@@ -713,6 +714,13 @@ pv_status transpose(pv_ctx *ctx, const turned *m, int n)
     return PV_OK;
 }
 
+// A tile's rows lie within 32 bits of its first: a row of an operand is below 16 MiB.  Asked before anything is enqueued.
+pv_status check_pitch(pv_ctx *ctx, int64_t bytes)
+{
+    if (bytes < 1 << 24) return PV_OK;
+    return pv_fail(ctx, PV_ERR_UNSUPPORTED, "a row of %lld bytes of an operand: 16 MiB or more", (long long)bytes);
+}
+
 // a matrix of codes as bf16 rows of whole blocks
 pv_status widen(pv_ctx *ctx, int format, const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *out)
 {
@@ -743,18 +751,20 @@ pv_status pv_launch_mx_product(pv_ctx *ctx, int64_t tokens, int64_t out, int64_t
     // scratch: both sides as bf16, or scales with rows of whole words; the splits' sums
     const int64_t pitch = (nblk + 3) & ~3, k = padded(in);
     const bool pad = !wide && pitch != nblk;
+    pv_status st = check_pitch(ctx, wide ? k * 2 : x_format == PV_MX_E2M1 ? k / 2 : k);
+    if (st != PV_OK) return st;
     const size_t wb = round16(wide ? (size_t)(out * k) * 2 : pad ? (size_t)(out * pitch) : 0);
     const size_t xb = round16(wide ? (size_t)(tokens * k) * 2 : pad ? (size_t)(tokens * pitch) : 0);
     void *scratch = nullptr;
     if (wb + xb + c.partial) {
-        const pv_status st = pv_ops_scratch(ctx, wb + xb + c.partial, &scratch);
+        st = pv_ops_scratch(ctx, wb + xb + c.partial, &scratch);
         if (st != PV_OK) return st;
     }
     uint8_t *ws = static_cast<uint8_t *>(scratch), *xs = ws + wb;
     float *partial = reinterpret_cast<float *>(xs + xb);
     pv_timed t(ctx, PV_K_MX_PRODUCT);
     if (wide) {
-        pv_status st = widen(ctx, PV_MX_E2M1, w_codes, w_scales, out, in, ws);
+        st = widen(ctx, PV_MX_E2M1, w_codes, w_scales, out, in, ws);
         if (st == PV_OK) st = widen(ctx, PV_MX_E4M3, x_codes, x_scales, tokens, in, xs);
         if (st != PV_OK) return st;
         return launch<kBF16, kBF16>(ctx, c, plain(ws, out, k), plain(xs, tokens, k), nblk, 0, partial, static_cast<float *>(Y));
@@ -767,7 +777,7 @@ pv_status pv_launch_mx_product(pv_ctx *ctx, int64_t tokens, int64_t out, int64_t
             PV_HIP(ctx, hipGetLastError());
             return PV_OK;
         };
-        pv_status st = words(w_scales, out, ws);
+        st = words(w_scales, out, ws);
         if (st == PV_OK) st = words(x_scales, tokens, xs);
         if (st != PV_OK) return st;
         w.scales = ws;
@@ -788,12 +798,14 @@ pv_status pv_launch_mx_product_grads(pv_ctx *ctx, int64_t tokens, int64_t out, i
 {
     const int64_t tp = padded(tokens), op = padded(out);
     const bool pad = dX && op != out;          // rows of dY that need an end
+    pv_status st = check_pitch(ctx, 2 * (dX && dW ? (op > tp ? op : tp) : dX ? op : tp));
+    if (st != PV_OK) return st;
     const choice cx = choose<kBF16, kBF16>(in, tokens, (int)(op / 32)), cw = choose<kBF16, kBF16>(in, out, (int)(tp / 32));
     // in order: the sums of either gradient | W^T, dY with padded rows | X^T, dY^T
     const size_t sums = round16(dX && cx.partial > (dW ? cw.partial : 0) ? cx.partial : dW ? cw.partial : 0);
     const int64_t wt = dX ? in * op : 0, dyp = pad ? tokens * op : 0, xt = dW ? in * tp : 0, dyt = dW ? out * tp : 0;
     void *p;
-    pv_status st = pv_ops_scratch(ctx, sums + (size_t)(wt + dyp + xt + dyt) * 2, &p);
+    st = pv_ops_scratch(ctx, sums + (size_t)(wt + dyp + xt + dyt) * 2, &p);
     if (st != PV_OK) return st;
     float *partial = static_cast<float *>(p);
     pv_bf16 *WT = reinterpret_cast<pv_bf16 *>(static_cast<uint8_t *>(p) + sums), *DYP = WT + wt, *XT = DYP + dyp, *DYT = XT + xt;

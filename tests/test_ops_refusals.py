@@ -119,6 +119,14 @@ def test_distill_outputs(lib, handle):
     refused(lib, handle, "pv_distill_topk_backward", (2, 9, 2, F32, A, 9, P, P, 1.0, P, P, None, 9), INVALID)
 
 
+def test_rows_of_16_mib_are_refused_before_anything_is_enqueued(lib, handle):
+    h, big, unsupported = handle[0], 1 << 24, 3
+    for args in ((17, 4, big, E4M3, P, P, P, P, BF16, P), (17, 4, 2 * big, E2M1, P, P, P, P, F32, P), (17, 4, big // 2, E4M3, P, P, P, P, F32, P)):
+        assert lib.pv_mx_product(h, *args) in (unsupported, 5)       # 5: there is no device here to make the context's
+    assert lib.pv_mx_product_grads(h, 4, big // 2, 4, E4M3, P, P, P, P, A, F32, B, None) in (unsupported, 5)
+    assert lib.pv_mx_product_grads(h, big // 2, 4, 4, E4M3, P, P, P, P, A, F32, None, C) in (unsupported, 5)
+
+
 def test_nothing_to_do_is_no_error(lib, handle):
     h = handle[0]
     assert lib.pv_quantize_mx(h, 0, 4, E2M1, F32, None, None, None) == OK
