@@ -59,7 +59,7 @@ __global__ __launch_bounds__(kBlock) void k_dequantize_mx(const uint8_t *__restr
     else c = reinterpret_cast<const pv_u2 *>(codes)[u];
     float v[8];
     pv_mx_decode<FMT>(c, pv_mx_power(scales[u >> 2]), v);
-    pv_store8(out + s.row * cols + (int64_t)s.unit * 8, s.valid, v);
+    pv_store8<true>(out + s.row * cols + (int64_t)s.unit * 8, s.valid, v);
 }
 
 __global__ __launch_bounds__(kBlock) void k_zero(uint16_t *p, int64_t n)

@@ -17,7 +17,7 @@ __device__ __forceinline__ void norm_out(const float (&v)[8], float rstd, const 
     float o[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = (v[i] * rstd) * w[i];
-    if (y) pv_store8(y + row * cols + (int64_t)unit * 8, valid, o);
+    if (y) pv_store8<true>(y + row * cols + (int64_t)unit * 8, valid, o);
     if (codes && unit < units) {
         const unsigned scale = pv_mx_scale<FMT>(pv_mx_largest(o));
         const pv_u2 c = pv_mx_encode<FMT>(o, scale);
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(TPR == 64 ? kBlock : TPR) void k_rms_norm(const T *
         if (row + stride < rows) load(row + stride);                // (another row: the outputs may lie on the inputs)
 #pragma unroll
         for (int u = 0; u < NV; ++u)
-            if (h) pv_store8(h + row * cols + (u * TPR + t) * 8, (int)cols - (u * TPR + t) * 8, v[u]);
+            if (h) pv_store8<true>(h + row * cols + (u * TPR + t) * 8, (int)cols - (u * TPR + t) * 8, v[u]);
         sum = pv_block_reduce<TPR>(sum, part[turn], pv_add{});
         const float rstd = 1.0f / sqrtf(sum / (float)cols + eps);
         if (rstd_out && t == 0) rstd_out[row] = rstd;
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(THREADS) void k_rms_norm_backward(const T *dy, cons
                 const float e = rstd * fmaf(-((float)b[u][i] * rstd), mean, (float)a[u][i] * w[u][i]);
                 d[i] = dh ? (float)c[u][i] + e : e;
             }
-            pv_store8(dx + row * cols + first, (int)cols - first, d);
+            pv_store8<true>(dx + row * cols + first, (int)cols - first, d);
         }
     }
     if (!partial) return;
