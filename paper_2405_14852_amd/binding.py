@@ -182,7 +182,7 @@ class PVContext:
             pass
 
     def _check(self, st: int):
-        if st != 0:
+        if st:
             raise PVError(st, self._lib.pv_last_error(self._h).decode())
 
     # ---- the four calls of the path -------------------------------------
@@ -321,9 +321,12 @@ class PVContext:
         if t is None and allow_none:
             return None
         # the checks of a call cost as much as a small kernel: those that pass are few and cheap
-        if (isinstance(t, torch.Tensor) and (t.dtype is dtype or (dtype is _DTYPES and t.dtype in dtype)) and t.shape == shape
-                and t.get_device() == self.device and t.is_contiguous()):
-            return t.data_ptr()
+        try:
+            if ((t.dtype is dtype or (dtype is _DTYPES and t.dtype in dtype)) and t.shape == shape
+                    and t.get_device() == self.device and t.is_contiguous()):
+                return t.data_ptr()
+        except AttributeError:
+            pass
         types = tuple(dtype) if dtype is _DTYPES else (dtype,)
         if isinstance(t, torch.Tensor) and t.dtype not in types:
             raise TypeError(f"{what} must be {' or '.join(map(str, types))}, got {t.dtype}")
@@ -370,21 +373,23 @@ class PVContext:
 
     def pv_rms_norm(self, rows: int, cols: int, x, residual, weight, eps: float, h=None, y=None, fmt: str = "e4m3",
                     codes=None, scales=None, rstd=None):
-        xp = self._tensor(x, _DTYPES, (rows, cols), "x")
-        same = lambda t, what: self._tensor(t, x.dtype, (rows, cols), what, allow_none=True)  # noqa: E731
-        c, s = self._coded(rows, cols, fmt, codes, scales, allow_none=True)
+        shape, tensor = (rows, cols), self._tensor
+        xp = tensor(x, _DTYPES, shape, "x")
+        dtype = x.dtype
+        c, s = (None, None) if codes is None and scales is None else self._coded(rows, cols, fmt, codes, scales, allow_none=True)
         self._check(self._lib.pv_rms_norm(
-            self._h, int(rows), int(cols), _DTYPES[x.dtype], xp, same(residual, "residual"),
-            self._tensor(weight, torch.float32, (cols,), "weight"), float(eps), same(h, "h"), same(y, "y"),
-            _mx_format(fmt), c, s, self._tensor(rstd, torch.float32, (rows,), "rstd", allow_none=True)))
+            self._h, int(rows), int(cols), _DTYPES[dtype], xp, tensor(residual, dtype, shape, "residual", True),
+            tensor(weight, torch.float32, (cols,), "weight"), float(eps), tensor(h, dtype, shape, "h", True),
+            tensor(y, dtype, shape, "y", True), _mx_format(fmt), c, s, tensor(rstd, torch.float32, (rows,), "rstd", True)))
 
     def pv_rms_norm_backward(self, rows: int, cols: int, dy, dh, h, weight, rstd, dx=None, dweight=None):
-        g = self._tensor(dy, _DTYPES, (rows, cols), "dy")
-        same = lambda t, what, none: self._tensor(t, dy.dtype, (rows, cols), what, allow_none=none)  # noqa: E731
+        shape, tensor = (rows, cols), self._tensor
+        g = tensor(dy, _DTYPES, shape, "dy")
+        dtype = dy.dtype
         self._check(self._lib.pv_rms_norm_backward(
-            self._h, int(rows), int(cols), _DTYPES[dy.dtype], g, same(dh, "dh", True), same(h, "h", False),
-            self._tensor(weight, torch.float32, (cols,), "weight"), self._tensor(rstd, torch.float32, (rows,), "rstd"),
-            same(dx, "dx", True), self._tensor(dweight, torch.float32, (cols,), "dweight", allow_none=True)))
+            self._h, int(rows), int(cols), _DTYPES[dtype], g, tensor(dh, dtype, shape, "dh", True), tensor(h, dtype, shape, "h"),
+            tensor(weight, torch.float32, (cols,), "weight"), tensor(rstd, torch.float32, (rows,), "rstd"),
+            tensor(dx, dtype, shape, "dx", True), tensor(dweight, torch.float32, (cols,), "dweight", True)))
 
     def _strided(self, t, dtype, rows: int, vocab: int, what: str):
         """Address and row stride of [rows, vocab] whose rows are dense."""
