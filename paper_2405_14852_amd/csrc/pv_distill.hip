@@ -269,14 +269,23 @@ pv_status pv_launch_distill(pv_ctx *ctx, int64_t rows, int64_t vocab, int k, int
         using T = decltype(v);
         const int units = (int)((vocab + unit_of<T>::n - 1) / unit_of<T>::n);
         auto launch = [&](auto kernel, int threads) {
-            const int64_t blocks = rows * a.pieces;
-            if (blocks >= (int64_t)1 << 31) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many rows of logits");
             if (lds > 65536 - 1024)
                 PV_HIP(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-            hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), lds, ctx->stream,
-                               static_cast<const T *>(logits), static_cast<T *>(grad), a);
-            PV_HIP(ctx, hipGetLastError());
+            // as many rows as a launch's threads, which are counted in 32 bits, allow
+            const int64_t most = ((int64_t)1 << 31) / threads / a.pieces;
+            for (int64_t row = 0; row < rows; row += most) {
+                args b = a;
+                b.ids += row * k;
+                b.top += row * k;
+                for (const float **q : {&b.row_weight, &b.lse_in})
+                    if (*q) *q += row;
+                for (float **q : {&b.loss, &b.lse})
+                    if (*q) *q += row;
+                hipLaunchKernelGGL(kernel, dim3((unsigned)((rows - row < most ? rows - row : most) * a.pieces)), dim3(threads), lds, ctx->stream,
+                                   static_cast<const T *>(logits) + row * ld, grad ? static_cast<T *>(grad) + row * grad_ld : nullptr, b);
+                PV_HIP(ctx, hipGetLastError());
+            }
             return PV_OK;
         };
         if (lse_in) {

@@ -646,12 +646,12 @@ pv_status launch_tiled(pv_ctx *ctx, const operand &w, const operand &x, tiling p
     p.wtiles = (w.rows + BM - 1) / BM;
     p.xtiles = (x.rows + BN - 1) / BN;
     const int64_t blocks = (int64_t)p.wtiles * p.xtiles * p.splits;
-    if (blocks >= (int64_t)1 << 31) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many tiles of the product");
+    if (!pv_grid_fits(blocks, WM * WN * 64)) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many tiles of the product");
     hipLaunchKernelGGL((k_product_tiled<WK, XK, BM, BN, WM, WN, NS, T>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0, ctx->stream, w, x, p, Y);
     PV_HIP(ctx, hipGetLastError());
     if (p.splits == 1) return PV_OK;
     const int64_t n = (int64_t)x.rows * w.rows, sums = (n + 2047) / 2048;
-    if (sums >= (int64_t)1 << 31) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many outputs of the product");
+    if (!pv_grid_fits(sums, 256)) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many outputs of the product");
     hipLaunchKernelGGL((k_add_splits<T>), dim3((unsigned)sums), dim3(256), 0, ctx->stream, p.partial, p.splits, n, Y);
     PV_HIP(ctx, hipGetLastError());
     return PV_OK;
@@ -662,7 +662,7 @@ pv_status launch_direct(pv_ctx *ctx, const operand &w, const operand &x, int nbl
 {
     const int wtiles = (w.rows + 15) / 16;
     const int64_t blocks = (int64_t)wtiles * ((x.rows + 15) / 16);
-    if (blocks >= (int64_t)1 << 31) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many tiles of the product");
+    if (!pv_grid_fits(blocks, 256)) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many tiles of the product");
     const bool few = blocks <= 512;
     const auto k = few ? k_product_direct<WIDE, WK, XK, 8, T> : k_product_direct<WIDE, WK, XK, 4, T>;
     hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(few ? 512 : 256), 0, ctx->stream, w, x, nblk, Y, wtiles);
@@ -708,7 +708,7 @@ pv_status transpose(pv_ctx *ctx, const turned *m, int n)
 {
     const turned none = {};
     const int64_t blocks = (int64_t)m[0].blocks + (n > 1 ? m[1].blocks : 0) + (n > 2 ? m[2].blocks : 0);
-    if (blocks >= (int64_t)1 << 31) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many tiles of the gradients' operands");
+    if (!pv_grid_fits(blocks, 256)) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many tiles of the gradients' operands");
     hipLaunchKernelGGL(k_transpose, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, m[0], n > 1 ? m[1] : none, n > 2 ? m[2] : none);
     PV_HIP(ctx, hipGetLastError());
     return PV_OK;
@@ -772,7 +772,7 @@ pv_status pv_launch_mx_product(pv_ctx *ctx, int64_t tokens, int64_t out, int64_t
     if (pad) {
         auto words = [&](const uint8_t *from, int64_t rows, uint8_t *to) {
             const int64_t blocks = (rows * (pitch / 4) + 255) / 256;
-            if (blocks >= (int64_t)1 << 31) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many scales");
+            if (!pv_grid_fits(blocks, 256)) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many scales");
             hipLaunchKernelGGL(k_pad_scales, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, from, rows, nblk, to, (int)pitch);
             PV_HIP(ctx, hipGetLastError());
             return PV_OK;
@@ -819,7 +819,7 @@ pv_status pv_launch_mx_product_grads(pv_ctx *ctx, int64_t tokens, int64_t out, i
     if (dX) {
         if (pad) {
             const int64_t blocks = (tokens * (op / 8) + 255) / 256;
-            if (blocks >= (int64_t)1 << 31) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many rows of dY");
+            if (!pv_grid_fits(blocks, 256)) return pv_fail(ctx, PV_ERR_UNSUPPORTED, "too many rows of dY");
             hipLaunchKernelGGL(k_pad_rows, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, static_cast<const pv_bf16 *>(dY),
                                tokens, out, DYP, op);
             PV_HIP(ctx, hipGetLastError());

@@ -91,34 +91,37 @@ __global__ __launch_bounds__(1024) void k_rms_norm_long(const T *x, const T *res
                                                         float *__restrict__ rstd_out, int64_t rows, int64_t cols,
                                                         int nblk)
 {
-    __shared__ float part[16];
-    const int64_t row = blockIdx.x, base = row * cols;
+    __shared__ float part[2][16];
     const int units = nblk * 4;
-    auto load = [&](int unit, int valid, float (&v)[8]) {
-        pv_load8(x + base + (int64_t)unit * 8, valid, v);
-        if (!residual) return;
-        float r[8];
-        pv_load8(residual + base + (int64_t)unit * 8, valid, r);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)(T)(v[i] + r[i]);
-    };
-    float sum = 0.0f;
-    for (int unit = threadIdx.x; unit < units; unit += 1024) {
-        float v[8];
-        load(unit, (int)cols - unit * 8, v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(v[i], v[i], sum);
-    }
-    sum = pv_block_reduce<1024>(sum, part, pv_add{});
-    const float rstd = 1.0f / sqrtf(sum / (float)cols + eps);
-    if (rstd_out && threadIdx.x == 0) rstd_out[row] = rstd;
-    for (int unit = threadIdx.x; unit < units; unit += 1024) {
-        const int valid = (int)cols - unit * 8;
-        float v[8], w[8];
-        load(unit, valid, v);
-        if (h) pv_store8(h + base + (int64_t)unit * 8, valid, v);
-        pv_load8(weight + (int64_t)unit * 8, valid, w);
-        norm_out<T, FMT>(v, rstd, w, valid, unit, units, row, cols, y, codes, scales);
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 1) {
+        const int64_t base = row * cols;
+        auto load = [&](int unit, int valid, float (&v)[8]) {
+            pv_load8(x + base + (int64_t)unit * 8, valid, v);
+            if (!residual) return;
+            float r[8];
+            pv_load8(residual + base + (int64_t)unit * 8, valid, r);
+    #pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = (float)(T)(v[i] + r[i]);
+        };
+        float sum = 0.0f;
+        for (int unit = threadIdx.x; unit < units; unit += 1024) {
+            float v[8];
+            load(unit, (int)cols - unit * 8, v);
+    #pragma unroll
+            for (int i = 0; i < 8; ++i) sum = fmaf(v[i], v[i], sum);
+        }
+        sum = pv_block_reduce<1024>(sum, part[turn], pv_add{});
+        const float rstd = 1.0f / sqrtf(sum / (float)cols + eps);
+        if (rstd_out && threadIdx.x == 0) rstd_out[row] = rstd;
+        for (int unit = threadIdx.x; unit < units; unit += 1024) {
+            const int valid = (int)cols - unit * 8;
+            float v[8], w[8];
+            load(unit, valid, v);
+            if (h) pv_store8(h + base + (int64_t)unit * 8, valid, v);
+            pv_load8(weight + (int64_t)unit * 8, valid, w);
+            norm_out<T, FMT>(v, rstd, w, valid, unit, units, row, cols, y, codes, scales);
+        }
     }
 }
 
@@ -304,7 +307,7 @@ pv_status pv_launch_rms_norm(pv_ctx *ctx, int64_t rows, int64_t cols, int type, 
         };
         if (units > kMostUnits) {
             const auto k = format == PV_MX_E2M1 ? k_rms_norm_long<T, PV_MX_E2M1> : k_rms_norm_long<T, PV_MX_E4M3>;
-            return launch(k, (unsigned)rows, 1024);
+            return launch(k, (unsigned)(rows < 4096 ? rows : 4096), 1024);
         }
         // short rows, enough of them to fill the chip: a wave a row
         if (units <= 128 && rows >= 1024) {

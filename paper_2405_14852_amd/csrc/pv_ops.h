@@ -11,6 +11,9 @@ constexpr int kMxBlock = 32;
 
 static inline int64_t pv_mx_blocks(int64_t cols) { return (cols + kMxBlock - 1) / kMxBlock; }
 
+// whether a launch can be made: its threads are counted in 32 bits
+static inline bool pv_grid_fits(int64_t blocks, int threads) { return blocks < ((int64_t)1 << 32) / threads; }
+
 static inline int pv_dtype_size(int t) { return t == PV_F32 ? 4 : 2; }
 
 // Scratch of these operators.  A block that a captured call has used stays until the context goes:

@@ -173,6 +173,27 @@ def test_no_entries_at_all(ctx):
     ctx.pv_distill_topk(0, 50, 0, torch.empty(0, 50, device=DEV), None, None, 1.0, loss=torch.empty(0, device=DEV))
 
 
+def test_more_rows_than_a_launch_has_blocks(ctx):
+    """2^32 threads are 2^24 rows of 256: the same as in parts."""
+    rows, half = (1 << 24) + 70, 1 << 23
+    g = torch.Generator(device=DEV).manual_seed(8)
+    z, top = torch.randn(rows, 3, generator=g, device=DEV), torch.randn(rows, 1, generator=g, device=DEV)
+    ids = torch.randint(0, 3, (rows, 1), generator=g, device=DEV, dtype=torch.int32)
+    c = torch.rand(rows, generator=g, device=DEV)
+    new = lambda n: (torch.empty(n, device=DEV), torch.empty(n, device=DEV), torch.empty(n, 3, device=DEV))  # noqa: E731
+    loss, lse, grad = new(rows)
+    ctx.pv_distill_topk(rows, 3, 1, z, ids, top, 2.0, row_weight=c, loss=loss, lse=lse, grad=grad)
+    back = torch.empty_like(grad)
+    ctx.pv_distill_topk_backward(rows, 3, 1, z, ids, top, 2.0, lse, c, back)
+    for at, n in [(0, half), (half, half), (2 * half, rows - 2 * half)]:
+        s = slice(at, at + n)
+        l2, e2, g2 = new(n)
+        ctx.pv_distill_topk(n, 3, 1, z[s], ids[s], top[s], 2.0, row_weight=c[s], loss=l2, lse=e2, grad=g2)
+        assert torch.equal(l2, loss[s]) and torch.equal(e2, lse[s]) and torch.equal(g2, grad[s])
+        ctx.pv_distill_topk_backward(n, 3, 1, z[s], ids[s], top[s], 2.0, e2, c[s], g2)
+        assert torch.equal(g2, back[s])
+
+
 def test_gradient_by_differences(ctx):
     """A central difference of the 64-bit loss along one direction."""
     rows, vocab, k, t = 4, 60, 7, 2.0

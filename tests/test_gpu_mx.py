@@ -105,6 +105,39 @@ def test_a_far_row_is_reached_with_64_bit_offsets(ctx):
     assert int(torch.count_nonzero(x[-1, :-32])) == 0 and int(torch.count_nonzero(x[0])) == 0
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("fmt", ["e2m1", "e4m3"])
+@pytest.mark.parametrize("rows,cols", [(1, 32), (77, 32), (1000, 64), (33, 96), (129, 128), (5, 160), (3, 1024), (2, 1056)])
+def test_rows_of_whole_blocks(ctx, rows, cols, fmt, dtype):
+    """One stretch after another whatever the rows; nothing is written behind the last."""
+    x = wild(rows, cols, dtype, seed=rows * 10007 + cols)
+    want_codes, want_scales = ref.quantize(x, fmt)
+    codes, scales = (torch.full((s[0] + 9, s[1]), 0xA5, dtype=torch.uint8, device=DEV) for s in mx_shapes(rows, cols, fmt))
+    ctx.pv_quantize_mx(rows, cols, fmt, x.to(DEV), codes[:rows], scales[:rows])
+    assert torch.equal(codes[:rows].cpu(), want_codes) and torch.equal(scales[:rows].cpu(), want_scales)
+    assert bool((codes[rows:] == 0xA5).all()) and bool((scales[rows:] == 0xA5).all())
+    out = torch.full((rows + 9, cols), 7.0, device=DEV)
+    ctx.pv_dequantize_mx(rows, cols, fmt, codes[:rows], scales[:rows], out[:rows])
+    assert torch.equal(out[:rows].cpu(), ref.decode(want_codes, want_scales, fmt, cols).float()) and bool((out[rows:] == 7.0).all())
+
+
+def test_more_short_rows_than_one_direction_of_a_grid_holds(ctx):
+    """A wave a row: 2^26 rows are 2^32 threads."""
+    rows, half = (1 << 26) + 70, 1 << 25
+    x = torch.randn(rows, 1, device=DEV).bfloat16()
+    codes, scales = (torch.full(s, 0xA5, dtype=torch.uint8, device=DEV) for s in mx_shapes(rows, 1, "e2m1"))
+    ctx.pv_quantize_mx(rows, 1, "e2m1", x, codes, scales)
+    for at, n in [(0, half), (half, half), (2 * half, rows - 2 * half)]:
+        c, s = coded(n, 1, "e2m1")
+        ctx.pv_quantize_mx(n, 1, "e2m1", x[at:at + n], c, s)
+        assert torch.equal(c, codes[at:at + n]) and torch.equal(s, scales[at:at + n])
+    out = torch.empty(rows, 1, dtype=torch.bfloat16, device=DEV)
+    ctx.pv_dequantize_mx(rows, 1, "e2m1", codes, scales, out)
+    tail = slice(rows - 200, rows)
+    assert torch.equal(out[tail].cpu(), ref.decode(*ref.quantize(x[tail].cpu(), "e2m1"), "e2m1", 1).bfloat16())
+    assert float((out.float() - x.float()).abs().max()) <= float(x.float().abs().max()) / 4     # E2M1's steps are a quarter of the value at most
+
+
 def operands(tokens, out, inn, fmt, seed):
     g = gen(seed)
     x = torch.randn(tokens, inn, generator=g) * torch.exp2(torch.randint(-3, 4, (tokens, 1), generator=g))

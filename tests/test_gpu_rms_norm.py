@@ -157,6 +157,24 @@ def test_backward_by_differences(ctx):
         assert abs(got - want) <= 1e-3 * 2.0 ** -4 * max(1.0, abs(want))
 
 
+def test_more_long_rows_than_blocks(ctx):
+    """Rows that no block holds in registers, more of them than a launch has blocks: the same as in parts, and in place."""
+    rows, cols = 4099, 16392
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.randn(rows, cols, generator=g, device=DEV).bfloat16()
+    weight = torch.rand(cols, generator=g, device=DEV) + 0.5
+    y, rstd = torch.empty_like(x), torch.empty(rows, device=DEV)
+    ctx.pv_rms_norm(rows, cols, x, x, weight, EPS, y=y, rstd=rstd)
+    for at, n in [(0, 2048), (2048, rows - 2048)]:
+        part, r = torch.empty(n, cols, dtype=x.dtype, device=DEV), torch.empty(n, device=DEV)
+        ctx.pv_rms_norm(n, cols, x[at:at + n], x[at:at + n], weight, EPS, y=part, rstd=r)
+        assert torch.equal(part, y[at:at + n]) and torch.equal(r, rstd[at:at + n])
+    want = ref.rms_norm(x[-3:], x[-3:], weight, EPS, x.dtype)[1]
+    ref.check(rstd[-3:], want, 1e-5 * want)
+    ctx.pv_rms_norm(rows, cols, x, x, weight, EPS, y=x)
+    assert torch.equal(x, y)
+
+
 def test_empty(ctx):
     e = lambda *s: torch.empty(*s, device=DEV)  # noqa: E731
     dw = torch.full((5,), 7.0, device=DEV)
