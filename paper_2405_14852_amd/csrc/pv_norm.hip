@@ -28,18 +28,18 @@ __device__ __forceinline__ void norm_out(const float (&v)[8], float rstd, const 
     }
 }
 
-// TPR threads share a row (64: kBlock / 64 rows a block, no barrier; else the block's), each with NV times eight values.  A block
+// TPR threads share a row (up to 64: kBlock / TPR rows a block, no barrier; else the block's), each with NV times eight values.  A block
 // goes from row to row, in steps of the grid, with its weights in registers and the next row already on its way while this
 // one is summed (8192 x 4096, bf16 to e4m3: 63.8 us with a wave a row and the weights read for each).
 template <class T, int TPR, int NV, int FMT>
-__global__ __launch_bounds__(TPR == 64 ? kBlock : TPR) void k_rms_norm(const T *x, const T *residual,
+__global__ __launch_bounds__(TPR <= 64 ? kBlock : TPR) void k_rms_norm(const T *x, const T *residual,
                                                                        const float *__restrict__ weight, float eps, T *h,
                                                                        T *y, uint8_t *__restrict__ codes,
                                                                        uint8_t *__restrict__ scales,
                                                                        float *__restrict__ rstd_out, int64_t rows,
                                                                        int64_t cols, int nblk)
 {
-    constexpr int kThreads = TPR == 64 ? kBlock : TPR, kRows = kThreads / TPR;
+    constexpr int kThreads = TPR <= 64 ? kBlock : TPR, kRows = kThreads / TPR;
     __shared__ float part[2][kThreads / 64];
     typedef typename pv_vec8<T>::raw raw;
     const int t = threadIdx.x % TPR, units = nblk * 4;
@@ -58,7 +58,7 @@ __global__ __launch_bounds__(TPR == 64 ? kBlock : TPR) void k_rms_norm(const T *
     float w[NV][8];
 #pragma unroll
     for (int u = 0; u < NV; ++u) pv_load8(weight + (u * TPR + t) * 8, (int)cols - (u * TPR + t) * 8, w[u]);
-    for (int turn = 0; row < rows; row += stride, turn ^= 1) {      // a whole wave's row, and a whole block's where it meets in barriers
+    for (int turn = 0; row < rows; row += stride, turn ^= 1) {      // alike in all that share a row, and a whole block's where it meets in barriers
         float v[NV][8], sum = 0.0f;
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
@@ -125,23 +125,26 @@ __global__ __launch_bounds__(1024) void k_rms_norm_long(const T *x, const T *res
     }
 }
 
-// Backward: block b takes the rows b, b + gridDim.x, ... with the weights and its sums for dweight in registers from row to
-// row; the sums leave once, as one row of `partial`.  A row stays as it was read, and the factors are formed twice, which takes
+// Backward: block b takes the rows b, b + gridDim.x, ... (short rows, of TPR threads: kRows of them at a time) with the weights and
+// its sums for dweight in registers from row to row; the sums leave once, as one row of `partial`.  A row stays as it was read, and the factors are formed twice, which takes
 // half the registers.  Where they leave room for one block a compute unit only and for another row (kAhead), that row is on its
 // way while this one is reduced.
-template <class T, int THREADS, int NV>
+template <class T, int THREADS, int NV, int TPR = THREADS>
 __global__ __launch_bounds__(THREADS) void k_rms_norm_backward(const T *dy, const T *dh, const T *h,
                                                                const float *__restrict__ weight,
                                                                const float *__restrict__ rstd_in, T *dx,
                                                                float *__restrict__ partial, int64_t rows, int64_t cols)
 {
+    constexpr int kRows = THREADS / TPR;
+    static_assert(kRows == 1 || (NV == 1 && TPR <= 64), "");
     __shared__ float part[2][THREADS / 64];
     typedef typename pv_vec8<T>::raw raw;
-    const int t = threadIdx.x;
+    const int t = threadIdx.x % TPR;
+    const int64_t row0 = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR, stride = (int64_t)gridDim.x * kRows;
     float acc[NV][8], w[NV][8];
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-        pv_load8(weight + (u * THREADS + t) * 8, (int)cols - (u * THREADS + t) * 8, w[u]);
+        pv_load8(weight + (u * TPR + t) * 8, (int)cols - (u * TPR + t) * 8, w[u]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[u][i] = 0.0f;
     }
@@ -150,21 +153,21 @@ __global__ __launch_bounds__(THREADS) void k_rms_norm_backward(const T *dy, cons
     auto load = [&](int64_t row, raw *a, raw *b, raw *c) {
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
-            const int first = (u * THREADS + t) * 8, valid = (int)cols - first;
+            const int first = (u * TPR + t) * 8, valid = (int)cols - first;
             a[u] = pv_load8_raw(dy + row * cols + first, valid);
             b[u] = pv_load8_raw(h + row * cols + first, valid);
             if (dh && dx) c[u] = pv_load8_raw(dh + row * cols + first, valid);
         }
     };
-    if constexpr (kAhead) load(blockIdx.x, next, next + NV, next + 2 * NV);
+    if constexpr (kAhead) load(row0, next, next + NV, next + 2 * NV);
     int turn = 0;
-    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 1) {
+    for (int64_t row = row0; row < rows; row += stride, turn ^= 1) {
         const float rstd = rstd_in[row];
         raw a[NV], b[NV], c[NV];
         if constexpr (kAhead) {
 #pragma unroll
             for (int u = 0; u < NV; ++u) a[u] = next[u], b[u] = next[NV + u], c[u] = next[2 * NV + u];
-            if (row + gridDim.x < rows) load(row + gridDim.x, next, next + NV, next + 2 * NV);      // (another row: dx may lie on an input)
+            if (row + stride < rows) load(row + stride, next, next + NV, next + 2 * NV);      // (another row: dx may lie on an input)
         } else {
             load(row, a, b, c);
         }
@@ -178,10 +181,10 @@ __global__ __launch_bounds__(THREADS) void k_rms_norm_backward(const T *dy, cons
                 dot = fmaf((float)a[u][i] * w[u][i], n, dot);
             }
         if (!dx) continue;
-        const float mean = pv_block_reduce<THREADS>(dot, part[turn], pv_add{}) / (float)cols;
+        const float mean = pv_block_reduce<TPR>(dot, part[turn], pv_add{}) / (float)cols;
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
-            const int first = (u * THREADS + t) * 8;
+            const int first = (u * TPR + t) * 8;
             float d[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -192,9 +195,22 @@ __global__ __launch_bounds__(THREADS) void k_rms_norm_backward(const T *dy, cons
         }
     }
     if (!partial) return;
+    if constexpr (kRows > 1) {                         // the block's rows together, in their order
+        __shared__ float s[kRows][TPR * 8 + 4];        // (16 bytes behind a row: its first bank is another's)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[threadIdx.x / TPR][t * 8 + i] = acc[0][i];
+        __syncthreads();
+        for (int col = threadIdx.x; col < TPR * 8 && col < cols; col += THREADS) {
+            float sum = s[0][col];
+#pragma unroll
+            for (int r = 1; r < kRows; ++r) sum += s[r][col];
+            partial[(int64_t)blockIdx.x * cols + col] = sum;
+        }
+        return;
+    }
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-        const int first = (u * THREADS + t) * 8;
+        const int first = (u * TPR + t) * 8;
         pv_store8(partial + (int64_t)blockIdx.x * cols + first, (int)cols - first, acc[u]);
     }
 }
@@ -250,22 +266,22 @@ __global__ __launch_bounds__(1024) void k_rms_norm_backward_long(const T *dy, co
     }
 }
 
-// dweight: the blocks' sums added in the order of the blocks, 8 threads a column for an eighth of them each
-__global__ __launch_bounds__(kBlock) void k_sum_partials(const float *__restrict__ partial, int parts, int64_t cols,
+// dweight: the blocks' sums added in the order of the blocks, 32 threads a column for a part of them each
+__global__ __launch_bounds__(1024) void k_sum_partials(const float *__restrict__ partial, int parts, int64_t cols,
                                                          float *__restrict__ out)
 {
-    __shared__ float s[8][32];
+    __shared__ float s[32][33];
     const int c = threadIdx.x & 31, e = threadIdx.x >> 5;
     const int64_t col = (int64_t)blockIdx.x * 32 + c;
     float sum = 0.0f;
     if (col < cols)
 #pragma unroll 8
-        for (int p = e * parts / 8; p < (e + 1) * parts / 8; ++p) sum += partial[(int64_t)p * cols + col];
+        for (int p = e * parts / 32; p < (e + 1) * parts / 32; ++p) sum += partial[(int64_t)p * cols + col];
     s[e][c] = sum;
     __syncthreads();
     if (e == 0 && col < cols) {
 #pragma unroll
-        for (int i = 1; i < 8; ++i) sum += s[i][c];
+        for (int i = 1; i < 32; ++i) sum += s[i][c];
         out[col] = sum;
     }
 }
@@ -309,15 +325,21 @@ pv_status pv_launch_rms_norm(pv_ctx *ctx, int64_t rows, int64_t cols, int type, 
             const auto k = format == PV_MX_E2M1 ? k_rms_norm_long<T, PV_MX_E2M1> : k_rms_norm_long<T, PV_MX_E4M3>;
             return launch(k, (unsigned)(rows < 4096 ? rows : 4096), 1024);
         }
-        // short rows, enough of them to fill the chip: a wave a row
+        // short rows, enough of them to fill the chip: a wave a row, or an eighth or a quarter of one (bf16, h and y: 2^20 rows of 64
+        // 314 us with a wave, 109 with a quarter, 83 with an eighth; 2^19 of 128 170 with a wave, 83 with a quarter)
         if (units <= 128 && rows >= 1024) {
-            const unsigned blocks = (unsigned)((rows + 3) / 4);
-            auto wave = [&](auto nv) {
-                constexpr int NV = decltype(nv)::value;
-                return launch(format == PV_MX_E2M1 ? k_rms_norm<T, 64, NV, PV_MX_E2M1> : k_rms_norm<T, 64, NV, PV_MX_E4M3>,
-                              blocks < 4096 ? blocks : 4096, kBlock);
+            auto wave = [&](auto lanes, auto nv) {
+                constexpr int NV = decltype(nv)::value, TPR = decltype(lanes)::value, kRows = kBlock / TPR;
+                const int64_t blocks = (rows + kRows - 1) / kRows;
+                return launch(format == PV_MX_E2M1 ? k_rms_norm<T, TPR, NV, PV_MX_E2M1> : k_rms_norm<T, TPR, NV, PV_MX_E4M3>,
+                              (unsigned)(blocks < 4096 ? blocks : 4096), kBlock);
             };
-            return units <= 64 ? wave(std::integral_constant<int, 1>{}) : wave(std::integral_constant<int, 2>{});
+            constexpr std::integral_constant<int, 1> one{};
+            constexpr std::integral_constant<int, 2> two{};
+            constexpr std::integral_constant<int, 8> eighth{};
+            constexpr std::integral_constant<int, 16> quarter{};
+            constexpr std::integral_constant<int, 64> whole{};
+            return units <= 8 ? wave(eighth, one) : units <= 16 ? wave(quarter, one) : units <= 32 ? wave(quarter, two) : units <= 64 ? wave(whole, one) : wave(whole, two);
         }
         auto block = [&](auto threads, auto nv) {
             constexpr int THREADS = decltype(threads)::value, NV = decltype(nv)::value;
@@ -337,7 +359,10 @@ pv_status pv_launch_rms_norm_backward(pv_ctx *ctx, int64_t rows, int64_t cols, i
     const int units = (int)((cols + 7) / 8);
     // each block leaves a row of sums that is written and read: no more of them than an eighth of the rows is worth
     const int64_t most = units > 1024 ? 256 : rows >= 4096 ? 1024 : 512;
-    const int64_t blocks = rows < most ? rows : most;
+    // threads a row of a block of 256: as many of 8, 16, 32, 64 as hold a short row, if there are enough of them to fill the chip
+    // (bf16, 2^19 rows of 128 with the block a row 1096 us, with 16 threads 99)
+    const int tpr = rows < 4096 || units > 64 ? 256 : units <= 8 ? 8 : units <= 16 ? 16 : units <= 32 ? 32 : 64;
+    const int64_t groups = (rows + 256 / tpr - 1) / (256 / tpr), blocks = groups < most ? groups : most;
     float *partial = nullptr;
     if (dweight && blocks > 1) {
         void *p;
@@ -358,11 +383,15 @@ pv_status pv_launch_rms_norm_backward(pv_ctx *ctx, int64_t rows, int64_t cols, i
             return PV_OK;
         };
         if (units > kMostUnits) return launch(k_rms_norm_backward_long<T>, 1024);
+        if (tpr == 8) return launch(k_rms_norm_backward<T, 256, 1, 8>, 256);
+        if (tpr == 16) return launch(k_rms_norm_backward<T, 256, 1, 16>, 256);
+        if (tpr == 32) return launch(k_rms_norm_backward<T, 256, 1, 32>, 256);
+        if (tpr == 64) return launch(k_rms_norm_backward<T, 256, 1, 64>, 256);
         if (units <= 256) return launch(k_rms_norm_backward<T, 256, 1>, 256);
         return for_nv<4>(units, 512, [&](auto nv) { return launch(k_rms_norm_backward<T, 512, decltype(nv)::value>, 512); });
     });
     if (st != PV_OK || partial == dweight) return st;
-    hipLaunchKernelGGL(k_sum_partials, dim3((unsigned)((cols + 31) / 32)), dim3(kBlock), 0, ctx->stream, partial,
+    hipLaunchKernelGGL(k_sum_partials, dim3((unsigned)((cols + 31) / 32)), dim3(1024), 0, ctx->stream, partial,
                        (int)blocks, cols, dweight);
     PV_HIP(ctx, hipGetLastError());
     return PV_OK;

@@ -176,21 +176,22 @@ __device__ __forceinline__ void pv_mx_decode(pv_u2 r, float power, float (&v)[8]
     }
 }
 
-template <class F>
+// over LANES neighbouring lanes
+template <int LANES = 64, class F>
 __device__ __forceinline__ float pv_wave_reduce(float v, F f)
 {
 #pragma unroll
-    for (int m = 32; m; m >>= 1) v = f(v, __shfl_xor(v, m));
+    for (int m = LANES / 2; m; m >>= 1) v = f(v, __shfl_xor(v, m));
     return v;
 }
 
-// over THREADS / 64 waves; `part` has one entry a wave and may be used again after another barrier
+// over THREADS / 64 waves, or a part of a wave; `part` has one entry a wave and may be used again after another barrier
 template <int THREADS, class F>
 __device__ __forceinline__ float pv_block_reduce(float v, float *part, F f)
 {
     constexpr int kWaves = THREADS / 64;
-    v = pv_wave_reduce(v, f);
-    if constexpr (kWaves == 1) return v;
+    v = pv_wave_reduce<(THREADS < 64 ? THREADS : 64)>(v, f);
+    if constexpr (kWaves <= 1) return v;
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
     __syncthreads();
     v = part[0];

@@ -157,6 +157,22 @@ def test_backward_by_differences(ctx):
         assert abs(got - want) <= 1e-3 * 2.0 ** -4 * max(1.0, abs(want))
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows,cols", [(1500, 64), (1025, 128), (1027, 31), (2000, 200), (1024, 256), (17001, 72), (1030, 257)])
+def test_many_short_rows(ctx, rows, cols, dtype):
+    """Several rows to a wave: heads' norms."""
+    test_norm(ctx, rows, cols, dtype, True)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows,cols", [(4096, 64), (4097, 128), (4111, 7), (4100, 200), (4098, 65), (5000, 500), (4097, 520), (20011, 33)])
+def test_backward_of_many_short_rows(ctx, rows, cols, dtype):
+    """A column's sum: R rows at a time (R = 32 at most, 4 at least) in P <= 1024 blocks, so ceil(rows / (R P)) + R + ceil(P / 32) + 32
+    additions one after the other; with P = 1024 only from 1024 R rows on.  At these shapes 86 at most (20011 rows of 33: R = 32,
+    P = 626), within the bound of the others, ceil(rows / 512) + 74, which is 82 or more and there 114."""
+    test_backward(ctx, rows, cols, dtype, True)
+
+
 def test_more_long_rows_than_blocks(ctx):
     """Rows that no block holds in registers, more of them than a launch has blocks: the same as in parts, and in place."""
     rows, cols = 4099, 16392
