@@ -177,8 +177,8 @@ __device__ __forceinline__ void pv_mx_decode(pv_u2 r, float power, float (&v)[8]
 }
 
 // over LANES neighbouring lanes
-template <int LANES = 64, class F>
-__device__ __forceinline__ float pv_wave_reduce(float v, F f)
+template <int LANES = 64, class V, class F>
+__device__ __forceinline__ V pv_wave_reduce(V v, F f)
 {
 #pragma unroll
     for (int m = LANES / 2; m; m >>= 1) v = f(v, __shfl_xor(v, m));
@@ -186,8 +186,8 @@ __device__ __forceinline__ float pv_wave_reduce(float v, F f)
 }
 
 // over THREADS / 64 waves, or a part of a wave; `part` has one entry a wave and may be used again after another barrier
-template <int THREADS, class F>
-__device__ __forceinline__ float pv_block_reduce(float v, float *part, F f)
+template <int THREADS, class V, class F>
+__device__ __forceinline__ V pv_block_reduce(V v, V *part, F f)
 {
     constexpr int kWaves = THREADS / 64;
     v = pv_wave_reduce<(THREADS < 64 ? THREADS : 64)>(v, f);
@@ -201,7 +201,8 @@ __device__ __forceinline__ float pv_block_reduce(float v, float *part, F f)
 }
 
 struct pv_add {
-    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+    template <class V>
+    __device__ __forceinline__ V operator()(V a, V b) const { return a + b; }
 };
 struct pv_max {
     __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }

@@ -173,6 +173,23 @@ def test_backward_of_many_short_rows(ctx, rows, cols, dtype):
     test_backward(ctx, rows, cols, dtype, True)
 
 
+@pytest.mark.parametrize("rows,cols", [(4096, 1024), (300, 16416)])
+def test_codes_are_those_of_the_formula(ctx, rows, cols):
+    """A value changes its code if it lies within its error of a tie, and ties lie an eighth of the value or more apart, so with an
+    error of 2^-24 of it one in 2^20 would.  The sum's error is what is left: eight terms of a lane in float32, 7 roundings of
+    at most half a 2^-23 each and of either sign, averaged over cols / 8 lanes and halved by the root: below 2^-24 * 7 / 2 / sqrt(cols / 8)
+    in the mean, 2^-26 here; one code in 2^22, so 1 is expected of 2^22, and 12 have a probability below 10^-8."""
+    g = torch.Generator(device=DEV).manual_seed(11)
+    x = (torch.randn(rows, cols, generator=g, device=DEV) * 3).bfloat16()
+    weight = 1 + 0.2 * torch.randn(cols, generator=g, device=DEV)
+    codes, scales = (torch.empty(s, dtype=torch.uint8, device=DEV) for s in mx_shapes(rows, cols, "e4m3"))
+    ctx.pv_rms_norm(rows, cols, x, None, weight, EPS, codes=codes, scales=scales)
+    _, _, y = ref.rms_norm(x, None, weight, EPS, x.dtype)
+    want_codes, want_scales = ref.quantize(y, "e4m3")
+    assert torch.equal(scales.cpu(), want_scales)
+    assert int((codes.cpu() != want_codes).sum()) <= 12
+
+
 def test_more_long_rows_than_blocks(ctx):
     """Rows that no block holds in registers, more of them than a launch has blocks: the same as in parts, and in place."""
     rows, cols = 4099, 16392
