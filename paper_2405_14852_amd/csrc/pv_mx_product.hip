@@ -228,12 +228,13 @@ __device__ __forceinline__ f16v multiply(const frag<WK> &w, unsigned ws, const f
 
 // BYTES (16 or 4) a lane from memory to LDS, lane i to `to` + BYTES * i.  An instruction and no builtin: behind the builtin the
 // compiler takes every later read of LDS for one that may be answered out of order, and waits for all of them at each use
-// (4096 x 8192 x 4096: 113 -> 107 us).  It has no result; the kernel waits for it by count.
+// (4096 x 8192 x 4096: 113 -> 107 us).  It has no result; the kernel waits for it by count.  It reads m0 one wait state after
+// a scalar instruction has written it at the earliest; the compiler, which counts those for its own instructions, does not look in here.
 template <int BYTES>
 __device__ __forceinline__ void fetch(const void *from, unsigned to)
 {
-    if constexpr (BYTES == 16) asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(to) : "memory");
-    else asm volatile("global_load_lds_dword %0, off" ::"v"(from), "{m0}"(to) : "memory");
+    if constexpr (BYTES == 16) asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(to) : "memory");
+    else asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "{m0}"(to) : "memory");
 }
 
 // All but the last N memory operations of this wave are done, its reads of LDS too, and every wave has come here.
