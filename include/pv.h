@@ -323,15 +323,12 @@ pv_status pv_dequantize_mx(pv_ctx *ctx, int64_t rows, int64_t cols, pv_mx_format
                            void *out);
 
 /* Y [tokens, out_features] = X W^T, both microscaled along in_features: X in x_format, W
- * [out_features, in_features] in PV_MX_E2M1.  Sums in fp32, rounded once to y_type.
- * Y in bf16 or f16, and any Y of X in E2M1: the scaled matrix instruction on the codes.  It cuts
- * products of E4M3 13 bits below the largest of 16 before it adds them (about 5e-6 of a sum of
- * normal data).  Y in f32 of X in E4M3: X and W take part as bf16, at half the rate, and nothing
- * is cut; bf16 holds every value of a code and a scale in [2^-117, 2^119] exactly, and the
- * quantisation makes no larger one.  in_features == 0 gives zeros.
+ * [out_features, in_features] in PV_MX_E2M1.  Sums in fp32, rounded once to y_type: the scaled
+ * matrix instruction on the codes, in two parts where X is in E4M3 (of which it would cut small
+ * products beside large ones).  in_features == 0 gives zeros.
  * More than 16 tokens: in_features < 2^23 (PV_ERR_UNSUPPORTED), and scratch of the context where
- * few tiles are many steps long (parts of the sums), where in_features is no multiple of 128 (the
- * scales) and for Y in f32 of X in E4M3 (both sides in bf16). */
+ * few tiles are many steps long (parts of the sums) and where in_features is no multiple of 128 (the
+ * scales). */
 pv_status pv_mx_product(pv_ctx *ctx, int64_t tokens, int64_t out_features, int64_t in_features,
                         pv_mx_format x_format, const uint8_t *x_codes, const uint8_t *x_scales,
                         const uint8_t *w_codes, const uint8_t *w_scales, pv_dtype y_type, void *Y);
@@ -340,7 +337,8 @@ pv_status pv_mx_product(pv_ctx *ctx, int64_t tokens, int64_t out_features, int64
  * quantisation unchanged (straight through):
  *   dX [tokens, in_features] of type dx_type = dY W           NULL ok
  *   dW f32 [out_features, in_features]       = dY^T X         NULL ok; the G of pv_encode_targets
- * W and X take part as bf16 (see above); sums in fp32.  The operands of a gradient that is not asked for are not read and may be
+ * W and X take part as bf16, which holds every value of a code and a scale in [2^-117, 2^119] exactly (the
+ * quantisation makes no larger one); sums in fp32.  The operands of a gradient that is not asked for are not read and may be
  * NULL (X for dX alone, W for dW alone).  The outputs are overwritten.  out_features < 2^23 for
  * dX, tokens < 2^23 for dW (PV_ERR_UNSUPPORTED).  Scratch of the context: W, X and dY transposed
  * in bf16, and parts of the sums. */

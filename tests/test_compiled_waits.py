@@ -1,5 +1,5 @@
-"""What the compiler does not count inside inline assembly: wait states between a scalar write of m0 and a load to LDS that reads it,
-in the code that is built from the sources here."""
+"""What the compiler does not count inside inline assembly, in the code that is built from the sources here: one wait state between a
+scalar write of m0 and a load to LDS that reads it, five between a vector instruction's write of a scalar and its use as an address."""
 import os
 import re
 import shutil
@@ -14,8 +14,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 
 def unwaited(assembly):
-    """Loads to LDS whose m0 was written by the instruction before."""
-    found, before, loads = [], "", 0
+    """Loads to LDS whose m0 was written by the instruction before, or whose address by one of the five before that are vector ones."""
+    found, before, loads, recent = [], "", 0, []
     for line in assembly.splitlines():
         text = line.split(";")[0].strip()
         if not text or text.startswith(".") or text.endswith(":"):
@@ -24,7 +24,13 @@ def unwaited(assembly):
             loads += 1
             if re.match(r"s_\w+ m0\b", before):
                 found.append((before, text))
+            address = re.search(r"s\[(\d+):(\d+)\]", text)
+            for past in recent[-5:] if address else ():
+                written = re.match(r"v_\w+ s\[?(\d+)(?::(\d+))?", past)
+                if written and int(written[1]) <= int(address[2]) and int(written[2] or written[1]) >= int(address[1]):
+                    found.append((past, text))
         before = text
+        recent.append(text)
     return loads, found
 
 
@@ -32,6 +38,9 @@ def test_the_check_sees_a_missing_wait():
     load = "\tglobal_load_lds_dwordx4 v1, s[2:3]\n"
     assert unwaited("\ts_mov_b32 m0, s4\n" + load) == (1, [("s_mov_b32 m0, s4", load.strip())])
     assert unwaited("\ts_add_i32 m0, s4, 16 ; comment\n\ts_nop 0\n" + load) == (1, [])
+    assert unwaited("\tv_readfirstlane_b32 s3, v4\n\ts_nop 3\n" + load) == (1, [("v_readfirstlane_b32 s3, v4", load.strip())])
+    assert unwaited("\tv_readfirstlane_b32 s4, v4\n\ts_nop 3\n" + load) == (1, [])
+    assert unwaited("\tv_readfirstlane_b32 s3, v4\n" + 5 * "\ts_nop 0\n" + load) == (1, [])
 
 
 @pytest.mark.skipif(not shutil.which(HIPCC), reason="no hipcc")

@@ -1,0 +1,89 @@
+"""The product's sums are float32 whatever the codes: nothing of a small product is lost beside a large one."""
+import pytest
+import torch
+
+import ops_reference as ref
+from paper_2405_14852_amd import PVContext, mx_shapes
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = PVContext(0)
+    yield c
+    c.close()
+
+
+def pack4(c):
+    return (c[:, 0::2] + 16 * c[:, 1::2]).to(torch.uint8)
+
+
+def cancelling(tokens, out, inn, seed):
+    """Codes of X (E4M3) and W (E2M1), all block scales 1.  A row of X holds one pair of neighbours of the largest value, W's columns
+    come in pairs of opposite sign, and all other values of X are below a quarter: the large products cancel and
+    the small ones are what is left.  All products are multiples of 2^-10, and their magnitudes add up to less than 2^14, so every
+    float32 sum of them is exact, in any order."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randint(0, 5 * 8, (tokens, inn), generator=g) + 128 * torch.randint(0, 2, (tokens, inn), generator=g)
+    w = torch.randint(0, 16, (out, inn), generator=g)
+    even = inn // 2 * 2
+    w[:, 1:even:2] = w[:, 0:even:2] ^ 8
+    at = torch.randint(0, even // 2, (tokens,), generator=g) * 2
+    rows = torch.arange(tokens)
+    x[rows, at], x[rows, at + 1] = 0x7e, 0x7e
+    pad = -inn % 32
+    x, w = torch.nn.functional.pad(x, (0, pad)), torch.nn.functional.pad(w, (0, pad))
+    xs, ws = (torch.full(mx_shapes(n, inn, "e4m3")[1], 127, dtype=torch.uint8) for n in (tokens, out))
+    return x.to(torch.uint8), xs, pack4(w), ws
+
+
+SHAPES = [(1, 40, 64), (3, 16, 100), (16, 130, 4096), (17, 70, 160), (40, 70, 4096), (100, 257, 1000), (300, 520, 2072), (1100, 1203, 300)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("tokens,out,inn", SHAPES)
+def test_small_products_beside_large_ones_that_cancel(ctx, tokens, out, inn, dtype):
+    xc, xs, wc, ws = cancelling(tokens, out, inn, seed=tokens + inn)
+    x, w = ref.decode(xc, xs, "e4m3", inn), ref.decode(wc, ws, "e2m1", inn)
+    assert float((x.abs() @ w.abs().T).max()) < 2.0 ** 14
+    y = torch.full((tokens, out), 7.0, dtype=dtype, device=DEV)
+    ctx.pv_mx_product(tokens, out, inn, "e4m3", *(t.to(DEV) for t in (xc, xs, wc, ws)), y)
+    want = (x @ w.T).float()                 # exact: one rounding is left, to the type
+    assert torch.equal(y.cpu(), want.to(dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("tokens,out,inn", [(5, 64, 512), (64, 200, 4096), (513, 300, 1056)])
+def test_codes_of_every_size(ctx, tokens, out, inn, dtype):
+    """Uniformly drawn codes reach over all of E4M3's powers of two.  An instruction adds its terms to a float32 sum and may lose 2^-22
+    of the magnitudes in it; each of 64 terms or more, and either half of the codes has its own."""
+    g = torch.Generator().manual_seed(inn)
+    x = torch.randint(0, 0x7f, (tokens, inn), generator=g) + 128 * torch.randint(0, 2, (tokens, inn), generator=g)
+    xc, wc = x.to(torch.uint8), pack4(torch.randint(0, 16, (out, inn), generator=g))
+    xs, ws = (torch.randint(116, 126, (n, inn // 32), generator=g).to(torch.uint8) for n in (tokens, out))
+    y = torch.full((tokens, out), 7.0, dtype=dtype, device=DEV)
+    x, w = ref.decode(xc, xs, "e4m3", inn), ref.decode(wc, ws, "e2m1", inn)
+    ctx.pv_mx_product(tokens, out, inn, "e4m3", *(t.to(DEV) for t in (xc, xs, wc, ws)), y)
+    want = x @ w.T
+    err = (2 * -(-inn // 64) + 8) * 2.0 ** -22 * (x.abs() @ w.abs().T)
+    over = torch.finfo(dtype).max
+    assert float((want.abs() + err).max()) < over
+    ref.check(y, want, err + ref.rounding(want.abs() + err, dtype))
+    # that bound is of the worst case; what is lost is of either sign: a step's loss is some 2^-24 of a sum's size
+    if dtype == torch.float32:
+        assert float((y.cpu().double() - want).norm() / want.norm()) <= 2.0 ** -20
+
+
+def test_every_product_is_of_the_codes_and_timed_once(ctx):
+    """No form converts its operands by another kernel: the product's bracket holds all of a call's time."""
+    xc, xs, wc, ws = (t.to(DEV) for t in cancelling(200, 300, 512, seed=3))
+    for dtype in TYPES:
+        y = torch.empty(200, 300, dtype=dtype, device=DEV)
+        ctx.pv_timing_enable(True)
+        ctx.pv_timing_reset()
+        ctx.pv_mx_product(200, 300, 512, "e4m3", xc, xs, wc, ws, y)
+        assert ctx.pv_timing_read("mx_product")[1] == 1 and ctx.pv_timing_read("mx_convert")[1] == 0
+        ctx.pv_timing_enable(False)
