@@ -160,10 +160,11 @@ __global__ __launch_bounds__(THREADS) void k_distill(const T *logits, T *grad, a
             if (atomicOr(&mark[id[j] >> 5], bit) & bit) s_twice = 1;
         }
     }
-    // q_v = exp2(z_v * scale - shift) / total, one operation an exponent; a rounded shift is the same in q and in the total.  A largest
-    // logit near the ends of float32 (a row masked by the type's lowest value) is subtracted first: its shift is not finite.
+    // q_v = exp2(z_v * scale - shift) / total, one operation an exponent; a rounded shift is the same in q and in the total.  What it
+    // is rounded by is a power of two in both: with a shift of 4096 or more (or one that is not finite) the largest logit is
+    // subtracted first.
     const float shift = top * scale;
-    const bool far = !(fabsf(top) < 1e30f);
+    const bool far = !(fabsf(shift) < 4096.0f);
     auto weight = [&](float x, auto is_far) {
         return __builtin_amdgcn_exp2f(decltype(is_far)::value ? (x - top) * scale : fmaf(x, scale, -shift));
     };

@@ -1,0 +1,109 @@
+"""Distillation of logits far from zero, of small temperatures and of far teachers: q and p depend on differences of logits alone,
+so what a row may be off does not grow with its distance from zero.  Against 64-bit sums of the differences."""
+import math
+
+import pytest
+import torch
+
+import ops_reference as ref
+from paper_2405_14852_amd import PVContext
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+U = 2.0 ** -24                      # half a step of float32
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = PVContext(0)
+    yield c
+    c.close()
+
+
+def expected(z, ids, top, t, weight=None):
+    """loss, lse, grad and what each may be off, row by row.  An exponent -(largest - z) / t of size d is formed by at most four
+    roundings, so its exponential is off by 4 d U of itself (d counts up to 104: what lies below is less than any float32);
+    a sum's terms pass as many additions as a lane has of them, and a tree's."""
+    z, u, ids, rows, vocab = z.double(), top.double(), ids.long(), z.shape[0], z.shape[1]
+    w = torch.ones(rows, dtype=torch.float64) if weight is None else weight.double()
+    there = (ids >= 0) & (ids < vocab)
+    at = torch.where(there, ids, 0)
+    u = torch.where(there, u, -math.inf)
+    big_z, big_u = z.amax(1, keepdim=True), u.amax(1, keepdim=True)
+    dz, du = (big_z - z) / t, torch.where(torch.isinf(u), math.inf, (big_u - u) / t)
+    any_ = big_u[:, 0] > -math.inf
+    sum_z, sum_u = torch.exp(-dz).sum(1, keepdim=True), torch.exp(-du).sum(1, keepdim=True)
+    q, p = torch.exp(-dz) / sum_z, torch.where(any_[:, None], torch.exp(-du) / sum_u, 0.0)
+    ln_q, ln_p = -dz.gather(1, at) - torch.log(sum_z), -du - torch.log(sum_u)
+    ratio = torch.where(p > 2.0 ** -149, ln_p - ln_q, 0.0)
+    on = (w != 0) & any_
+    loss = torch.where(on, w * t * t * (p * ratio).sum(1), 0.0)
+    lse = torch.where(w != 0, big_z[:, 0] / t + torch.log(sum_z)[:, 0], 0.0)
+    target = torch.zeros_like(z).scatter_add(1, at, torch.where(there, p, 0.0))
+    grad = torch.where(on[:, None], (w * t)[:, None] * (q - target), 0.0)
+    lane = max(256, -(-vocab // 512) * 5 // 4)
+    depth = lambda d: torch.where(d < 104, d, 0.0).amax(1)  # noqa: E731
+    s_z, s_u = (4 * depth(dz) + lane + 24) * U, (4 * depth(du) + 40) * U
+    off_lse = s_z + lse.abs() * 4 * U
+    size = (p * ratio.abs()).sum(1)
+    off_loss = w.abs() * t * t * (s_z + s_u + (s_u + 32 * U) * size + 8 * U * (1 + (p * torch.where(p > 2.0 ** -149, dz.gather(1, at) + du, 0.0)).sum(1)))
+    off_grad = (w.abs() * t)[:, None] * ((s_z + 8 * U)[:, None] * q + (s_u + 24 * U)[:, None] * target) + 2.0 ** -120
+    # nothing here allows more than a few digits of float32: no row hides behind another's size
+    assert float(s_z.max()) < 2.0 ** -13 and float(s_u.max()) < 2.0 ** -14
+    return (loss, lse, grad), (off_loss, off_lse, off_grad)
+
+
+def compare(ctx, z, ids, top, t, weight=None, backward=True):
+    rows, vocab, k, dtype = z.shape[0], z.shape[1], ids.shape[1], z.dtype
+    args = (rows, vocab, k, z.to(DEV), ids.to(DEV), top.to(DEV), t)
+    wd = None if weight is None else weight.to(DEV)
+    (loss, lse, grad), (off_loss, off_lse, off_grad) = expected(z, ids, top, t, weight)
+    got_loss, got_lse = torch.full((rows,), 7.0, device=DEV), torch.full((rows,), 7.0, device=DEV)
+    got = torch.full((rows, vocab), 7.0, dtype=dtype, device=DEV)
+
+    def check(got, want, off, what):
+        ref.check(got, want, off + ref.rounding(want.abs() + off, got.dtype), what)
+
+    beyond = lse.abs() > torch.finfo(torch.float32).max
+    lse = torch.where(beyond, lse.sign() * math.inf, lse)
+    off_lse = torch.where(beyond, 0.0, off_lse)
+    for g in (got, None):
+        ctx.pv_distill_topk(*args, row_weight=wd, loss=got_loss, lse=got_lse, grad=g)
+        check(got_loss, loss, off_loss, "loss")
+        ref.check(got_lse, lse, off_lse, "lse")
+    check(got, grad, off_grad, "grad")
+    if not backward:
+        return
+    # the two directions agree: from the saved sum, for a gradient of the loss that is this call's weight
+    ctx.pv_distill_topk(*args, loss=got_loss, lse=got_lse)
+    w = torch.linspace(0.5, 1.5, rows) if weight is None else weight
+    (_, lse, grad), (_, _, off_grad) = expected(z, ids, top, t, w)
+    # up to 256 the saved float32 sum is off by 2 U of itself, and so is every z / t: q follows
+    near = torch.where(lse.abs() < 256, 2 * (lse.abs() + (lse.abs() + 104)) * 2 * U, 0.0)
+    off_grad = off_grad + (w.double().abs() * t * near)[:, None] * torch.softmax((z.double() - z.double().amax(1, keepdim=True)) / t, 1)
+    for place in (torch.full_like(got, 9.0), args[3]):              # (the last in place of the logits)
+        ctx.pv_distill_topk_backward(*args, got_lse, w.to(DEV), place)
+        check(place, grad, off_grad, "backward")
+
+
+FAR = [0.0, 2000.0, -1e4, 6e4, 1e6, -1e6, -1e9, 1e9, 4e9, -1e10, -1e12, -1e20, 1e20, -1e29, 1e31, -3e38]
+
+
+def far_rows(vocab, dtype, seed):
+    """Two rows at each distance from zero that the type holds: of one value, and of values around it (as far as the type tells them
+    apart)."""
+    g = torch.Generator().manual_seed(seed)
+    at = [b for b in FAR if abs(b) < torch.finfo(dtype).max]
+    z = torch.cat([torch.stack((torch.full((vocab,), b, dtype=torch.float64), b + 2.5 * torch.randn(vocab, generator=g, dtype=torch.float64)))
+                   for b in at]).to(dtype)
+    k = min(vocab, 6)
+    ids = torch.stack([torch.randperm(vocab, generator=g)[:k] for _ in z]).int()
+    return z, ids, torch.randn(len(z), k, generator=g) * 2
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("vocab", [1, 50, 3001, 9000, 33000])
+def test_rows_far_from_zero(ctx, vocab, dtype):
+    """Rows that stay in registers."""
+    compare(ctx, *far_rows(vocab, dtype, seed=vocab), 1.0, backward=False)
