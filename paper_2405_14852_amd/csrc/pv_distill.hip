@@ -162,9 +162,9 @@ __global__ __launch_bounds__(THREADS) void k_distill(const T *logits, T *grad, a
     }
     // q_v = exp2(z_v * scale - shift) / total, one operation an exponent; a rounded shift is the same in q and in the total.  What it
     // is rounded by is a power of two in both: with a shift of 4096 or more (or one that is not finite) the largest logit is
-    // subtracted first.
+    // subtracted first.  So it is in rows that pass by: their total was, and has nothing of a rounded shift.
     const float shift = top * scale;
-    const bool far = !(fabsf(shift) < 4096.0f);
+    const bool far = (NV == 0 && !LSE) || !(fabsf(shift) < 4096.0f);
     auto weight = [&](float x, auto is_far) {
         return __builtin_amdgcn_exp2f(decltype(is_far)::value ? (x - top) * scale : fmaf(x, scale, -shift));
     };
@@ -219,8 +219,8 @@ __global__ __launch_bounds__(THREADS) void k_distill(const T *logits, T *grad, a
         }
     }
     if constexpr (!LSE) {
-        // where the rounded shift was subtracted, the total is off by what it was rounded by (of a register row; 6e-8 of the largest logit)
-        const float log_total = logf(total) - (NV == 0 || far ? 0.0f : fmaf(top, scale, -shift) * 0.69314718055994530942f);
+        // where the rounded shift was subtracted, the total is off by what it was rounded by (6e-8 of the largest logit)
+        const float log_total = logf(total) - (far ? 0.0f : fmaf(top, scale, -shift) * 0.69314718055994530942f);
         float loss = 0.0f;
         for (int j = tid; j < k; j += THREADS) {
             const float pj = p_of(j);

@@ -107,3 +107,10 @@ def far_rows(vocab, dtype, seed):
 def test_rows_far_from_zero(ctx, vocab, dtype):
     """Rows that stay in registers."""
     compare(ctx, *far_rows(vocab, dtype, seed=vocab), 1.0, backward=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("vocab", [70000, 140001])
+def test_long_rows_far_from_zero(ctx, vocab, dtype):
+    """Rows that pass by (70000 of 16 bits still stay): the gradient belongs to the same sum as the loss."""
+    compare(ctx, *far_rows(vocab, dtype, seed=vocab), 1.0, backward=False)
