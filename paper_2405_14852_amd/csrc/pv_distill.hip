@@ -63,7 +63,7 @@ __global__ __launch_bounds__(THREADS) void k_distill(const T *logits, T *grad, a
     typedef typename unit_of<T>::raw raw;
     typedef typename unit_of<T>::type loose;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    float *p = reinterpret_cast<float *>(lds);                        // [k] the teacher's logits by the temperature
+    float *p = reinterpret_cast<float *>(lds);                        // [k] the teacher's logits
     float *zt = p + a.k;                                              // [k] the logits in their places
     int *id = reinterpret_cast<int *>(zt + a.k);                      // [k] their places, -1: none
     unsigned *mark = reinterpret_cast<unsigned *>(id + a.k);          // [ceil(vocab / 32)] places of the row
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(THREADS) void k_distill(const T *logits, T *grad, a
     for (int j = tid; j < k; j += THREADS) {
         const int i = a.ids[row * k + j];
         const bool in = i >= 0 && i < V;
-        const float u = in ? a.top[row * k + j] * inv_t : kNone;
+        const float u = in ? a.top[row * k + j] : kNone;
         id[j] = in ? i : -1;
         p[j] = u;
         zt[j] = in ? (float)z[i] : 0.0f;
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(THREADS) void k_distill(const T *logits, T *grad, a
     for (int j = tid; j < k; j += THREADS) {
         if (id[j] < 0) continue;
         const float u = p[j];
-        sum_u += max_u > kNone || u != u ? expf(u - max_u) : 0.0f;
+        sum_u += max_u > kNone || u != u ? expf((u - max_u) * inv_t) : 0.0f;
         if (g) {
             const unsigned bit = 1u << (id[j] & 31);
             if (atomicOr(&mark[id[j] >> 5], bit) & bit) s_twice = 1;
@@ -183,11 +183,11 @@ __global__ __launch_bounds__(THREADS) void k_distill(const T *logits, T *grad, a
         total *= __builtin_amdgcn_exp2f((own_top - top) * scale);
     }
     reduce_two<kWaves>(total, sum_u, part[1], pv_add{});
-    // p_j = exp(u_j - max_u - log_sum_u); q_v as above, or exp(z_v / t - lse) with the sum given
+    // p_j = exp((u_j - max_u) / t - log_sum_u); q_v as above, or exp(z_v / t - lse) with the sum given
     const bool any = sum_u != 0.0f;               // (of the largest entry's 1, unless there is none)
     const float log_sum_u = logf(sum_u), inv_total = 1.0f / total, lse = LSE ? a.lse_in[row] : 0.0f;
     const float factor = any ? c * a.t : 0.0f;
-    auto p_of = [&](int j) { return any && id[j] >= 0 ? expf(p[j] - max_u - log_sum_u) : 0.0f; };
+    auto p_of = [&](int j) { return any && id[j] >= 0 ? expf((p[j] - max_u) * inv_t - log_sum_u) : 0.0f; };
     const float factor_q = LSE ? factor : factor * inv_total;
     auto grad_q = [&](float x, auto is_far) {
         if constexpr (LSE) return factor_q * __builtin_amdgcn_exp2f(fmaf(x, inv_t, -lse) * kLog2e);
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(THREADS) void k_distill(const T *logits, T *grad, a
         float loss = 0.0f;
         for (int j = tid; j < k; j += THREADS) {
             const float pj = p_of(j);
-            if (pj != 0.0f) loss = fmaf(pj, ((p[j] - max_u - log_sum_u) - (zt[j] - top) * inv_t) + log_total, loss);
+            if (pj != 0.0f) loss = fmaf(pj, (((p[j] - max_u) * inv_t - log_sum_u) - (zt[j] - top) * inv_t) + log_total, loss);
         }
         loss = pv_block_reduce<THREADS>(loss, part[2], pv_add{});
         if (tid == 0) {

@@ -114,3 +114,17 @@ def test_rows_far_from_zero(ctx, vocab, dtype):
 def test_long_rows_far_from_zero(ctx, vocab, dtype):
     """Rows that pass by (70000 of 16 bits still stay): the gradient belongs to the same sum as the loss."""
     compare(ctx, *far_rows(vocab, dtype, seed=vocab), 1.0, backward=False)
+
+
+@pytest.mark.parametrize("t", [0.25, 1.0, 3.0])
+@pytest.mark.parametrize("vocab", [50, 70000])
+def test_teachers_far_from_zero(ctx, vocab, t):
+    """The teacher's logits are shifted, one value, or at either end of float32."""
+    z, ids, top = far_rows(vocab, torch.float32, seed=9)
+    low, high = torch.finfo(torch.float32).min, torch.finfo(torch.float32).max
+    for r, b in enumerate([1e3, -1e4, 1e6, -1e6, 1e9, -1e9, 1e20, -1e30]):
+        top[r] = (top[r].double() + b).float()
+    top[8], top[9], top[10, 1:], top[11, ::2] = low, high, low, high
+    top[12, 0], top[12, 1] = high, low
+    top[13], top[13, 2] = -math.inf, -1e38
+    compare(ctx, z[:16], ids[:16], top[:16], t, backward=False)
