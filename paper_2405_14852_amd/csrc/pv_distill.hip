@@ -221,14 +221,15 @@ __global__ __launch_bounds__(THREADS) void k_distill(const T *logits, T *grad, a
     if constexpr (!LSE) {
         // where the rounded shift was subtracted, the total is off by what it was rounded by (6e-8 of the largest logit)
         const float log_total = logf(total) - (far ? 0.0f : fmaf(top, scale, -shift) * 0.69314718055994530942f);
+        // t (ln p - ln q), whose differences of logits need no division: nothing leaves float32 at a small t, and t^2 is not formed
         float loss = 0.0f;
         for (int j = tid; j < k; j += THREADS) {
             const float pj = p_of(j);
-            if (pj != 0.0f) loss = fmaf(pj, (((p[j] - max_u) * inv_t - log_sum_u) - (zt[j] - top) * inv_t) + log_total, loss);
+            if (pj != 0.0f) loss = fmaf(pj, fmaf(a.t, log_total - log_sum_u, (p[j] - max_u) - (zt[j] - top)), loss);
         }
         loss = pv_block_reduce<THREADS>(loss, part[2], pv_add{});
         if (tid == 0) {
-            a.loss[row] = any ? c * a.t * a.t * loss : 0.0f;
+            a.loss[row] = any ? c * a.t * loss : 0.0f;
             if (a.lse) a.lse[row] = top * inv_t + log_total;
         }
     }

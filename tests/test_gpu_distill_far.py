@@ -110,6 +110,16 @@ def test_rows_far_from_zero(ctx, vocab, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("t", [2.0 ** -126, 1e-30, 1e-12, 1e-9, 1e-6, 0.01, 100.0])
+def test_small_and_large_temperatures(ctx, t, dtype):
+    """Of the largest logits alone, or nearly uniform."""
+    t = float(torch.tensor(t, dtype=torch.float32))
+    z, ids, top = far_rows(700, dtype, seed=5)
+    z[:, 100:103] = z.amax(1, keepdim=True)                          # some places share the probability
+    compare(ctx, z, ids, top, t, backward=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("vocab", [70000, 140001])
 def test_long_rows_far_from_zero(ctx, vocab, dtype):
     """Rows that pass by (70000 of 16 bits still stay): the gradient belongs to the same sum as the loss."""
