@@ -386,7 +386,7 @@ pv_status pv_rms_norm_backward(pv_ctx *ctx, int64_t rows, int64_t cols, pv_dtype
  * logits [rows, vocab], row stride ld >= vocab elements; grad alike with grad_ld, and may be logits
  * (same pointer and stride): behind a row's vocab elements nothing is read or written.
  * teacher_ids i32 [rows, k], teacher_logits f32 [rows, k].  0 <= k <= 1024, 1 <= vocab <= 2^20,
- * temperature > 0. */
+ * 2^-126 <= temperature <= 2^63. */
 pv_status pv_distill_topk(pv_ctx *ctx, int64_t rows, int64_t vocab, int32_t k, pv_dtype type,
                           const void *logits, int64_t ld, const int32_t *teacher_ids,
                           const float *teacher_logits, float temperature,

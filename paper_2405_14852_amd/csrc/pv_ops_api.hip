@@ -193,7 +193,8 @@ static pv_status check_distill(pv_ctx *ctx, int64_t rows, int64_t vocab, int32_t
     PV_CHECK(check_enums(ctx, type, PV_MX_E4M3));
     if (vocab < 1 || vocab > 1 << 20) return pv_fail(ctx, PV_ERR_SHAPE, "vocab %lld not in 1..2^20", (long long)vocab);
     if (k < 0 || k > 1024) return pv_fail(ctx, PV_ERR_INVALID_ARG, "k = %d not in 0..1024", k);
-    if (!(temperature > 0.0f && temperature < INFINITY)) return pv_fail(ctx, PV_ERR_INVALID_ARG, "temperature must be positive and finite");
+    // (its reciprocal is a normal number, and so is its square, which the loss is a part of)
+    if (!(temperature >= 0x1p-126f && temperature <= 0x1p63f)) return pv_fail(ctx, PV_ERR_INVALID_ARG, "temperature not in 2^-126..2^63");
     if (ld < vocab || (grad && grad_ld < vocab)) return pv_fail(ctx, PV_ERR_SHAPE, "a row stride is below vocab");
     if (ld >= (int64_t)1 << 40 || (grad && grad_ld >= (int64_t)1 << 40) || rows * (ld >> 20) >= (int64_t)1 << 40)
         return pv_fail(ctx, PV_ERR_SHAPE, "row stride too large");
