@@ -395,7 +395,8 @@ pv_status pv_distill_topk(pv_ctx *ctx, int64_t rows, int64_t vocab, int32_t k, p
 
 /* The gradient alone, of a forward call without row_weight, for d phi / d loss given afterwards:
  *   grad_v = grad_loss * t * (q_v - sum over j with id_j == v of p_j),  q_v = exp(z_v / t - lse)
- * lse f32 [rows] as pv_distill_topk wrote it; grad_loss f32 [rows]: a row of 0 is not read, its
+ * lse f32 [rows] as pv_distill_topk wrote it; of a row whose |lse| is 256 or more (or no number) the sum
+ * is formed again from its logits, since a float32 lse no longer holds it.  grad_loss f32 [rows]: a row of 0 is not read, its
  * gradient is 0. */
 pv_status pv_distill_topk_backward(pv_ctx *ctx, int64_t rows, int64_t vocab, int32_t k,
                                    pv_dtype type, const void *logits, int64_t ld,

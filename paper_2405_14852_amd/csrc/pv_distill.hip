@@ -22,6 +22,20 @@ struct unit_of {                                  // 16 bytes of a row, at any e
     typedef raw type __attribute__((aligned(sizeof(T))));
 };
 
+// past the caches (2048 x 32000: 61.5 -> 56.2 us)
+template <class T>
+__device__ __forceinline__ void store_unit(T *g, int unit, int vocab, const typename unit_of<T>::raw &r)
+{
+    constexpr int U = unit_of<T>::n;
+    if ((unit + 1) * U <= vocab) {
+        __builtin_nontemporal_store(r, reinterpret_cast<typename unit_of<T>::type *>(g + unit * U));
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+        if (unit * U + i < vocab) g[unit * U + i] = r[i];
+}
+
 // two values over a block, with one barrier
 template <int WAVES, class F>
 __device__ __forceinline__ void reduce_two(float &a, float &b, float *part, F f)
@@ -55,8 +69,9 @@ struct args {
 // NV > 0: the row lies in NV units a thread.  NV == 0: it passes by, with a running largest value and sum in each thread, and
 // is read again for the gradient if there is one.
 // LSE: the sum is given (the backward call), only the gradient is formed, by a block for every NV units a thread of a row.
+// row, z, g: the block's row; c: its weight; first: the unit that the block begins with.
 template <class T, int THREADS, int NV, bool LSE>
-__global__ __launch_bounds__(THREADS) void k_distill(const T *logits, T *grad, args a)
+__device__ __forceinline__ void distill_row(const args &a, int64_t row, const T *z, T *g, float c, int first)
 {
     constexpr int U = unit_of<T>::n, kWaves = THREADS / 64;
     constexpr float kNone = -__builtin_inff();
@@ -71,11 +86,6 @@ __global__ __launch_bounds__(THREADS) void k_distill(const T *logits, T *grad, a
     __shared__ int s_twice;                                           // some place has two entries
 
     const int tid = threadIdx.x, V = a.vocab, k = a.k;
-    const int64_t row = LSE ? blockIdx.x / a.pieces : blockIdx.x;
-    const int first = LSE ? (int)(blockIdx.x % a.pieces) * (NV * THREADS) : 0;      // unit of this block
-    const T *z = logits + row * a.ld;
-    T *g = grad ? grad + row * a.grad_ld : nullptr;
-    const float c = a.row_weight ? a.row_weight[row] : 1.0f;
     const int units = LSE ? min((V + U - 1) / U, first + NV * THREADS) : (V + U - 1) / U;
 
     auto load = [&](int unit) {
@@ -85,26 +95,7 @@ __global__ __launch_bounds__(THREADS) void k_distill(const T *logits, T *grad, a
         for (int i = 0; i < U; ++i) r[i] = unit * U + i < V ? z[unit * U + i] : (T)kNone;
         return r;
     };
-    auto store = [&](int unit, const raw &r) {
-        if ((unit + 1) * U <= V) {
-            __builtin_nontemporal_store(r, reinterpret_cast<loose *>(g + unit * U));      // (2048 x 32000: 61.5 -> 56.2 us)
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < U; ++i)
-            if (unit * U + i < V) g[unit * U + i] = r[i];
-    };
-
-    if (c == 0.0f) {
-        const raw zero = {};
-        if (g)
-            for (int unit = first + tid; unit < units; unit += THREADS) store(unit, zero);
-        if (tid == 0 && !LSE) {
-            a.loss[row] = 0.0f;
-            if (a.lse) a.lse[row] = 0.0f;
-        }
-        return;
-    }
+    auto store = [&](int unit, const raw &r) { store_unit(g, unit, V, r); };
 
     raw v[NV ? NV : 1];
     if constexpr (NV > 0) {
@@ -228,7 +219,7 @@ __global__ __launch_bounds__(THREADS) void k_distill(const T *logits, T *grad, a
             if (pj != 0.0f) loss = fmaf(pj, fmaf(a.t, log_total - log_sum_u, (p[j] - max_u) - (zt[j] - top)), loss);
         }
         loss = pv_block_reduce<THREADS>(loss, part[2], pv_add{});
-        if (tid == 0) {
+        if (tid == 0 && a.loss) {
             a.loss[row] = any ? c * a.t * loss : 0.0f;
             if (a.lse) a.lse[row] = top * inv_t + log_total;
         }
@@ -256,6 +247,40 @@ __global__ __launch_bounds__(THREADS) void k_distill(const T *logits, T *grad, a
         }
         if (place >= first * U && place < units * U) g[place] = (T)((far ? grad_q(zt[e], std::true_type{}) : grad_q(zt[e], std::false_type{})) - factor * sum);
     }
+}
+
+// A saved sum of this size or more is off by 2^-16 and more of what it should be in q, as a float32 logarithm has no more digits, and
+// of a row of one far value it has none of the vocabulary's logarithm.
+constexpr float kFarSum = 256.0f;
+
+template <class T, int THREADS, int NV, bool LSE>
+__global__ __launch_bounds__(THREADS) void k_distill(const T *logits, T *grad, args a)
+{
+    constexpr int U = unit_of<T>::n;
+    const int64_t row = LSE ? blockIdx.x / a.pieces : blockIdx.x;
+    const int first = LSE ? (int)(blockIdx.x % a.pieces) * (NV * THREADS) : 0;      // unit of this block
+    const T *z = logits + row * a.ld;
+    T *g = grad ? grad + row * a.grad_ld : nullptr;
+    const float c = a.row_weight ? a.row_weight[row] : 1.0f;
+    if (c == 0.0f) {
+        const int all = (a.vocab + U - 1) / U, units = LSE ? min(all, first + NV * THREADS) : all;
+        const typename unit_of<T>::raw zero = {};
+        if (g)
+            for (int unit = first + threadIdx.x; unit < units; unit += THREADS) store_unit(g, unit, a.vocab, zero);
+        if (threadIdx.x == 0 && !LSE) {
+            a.loss[row] = 0.0f;
+            if (a.lse) a.lse[row] = 0.0f;
+        }
+        return;
+    }
+    if constexpr (LSE) {
+        if (!(fabsf(a.lse_in[row]) < kFarSum)) {
+            // the row's first block forms the sum again and the gradient of all of it; no other touches the row
+            if (first == 0) distill_row<T, THREADS, 0, false>(a, row, z, g, c, 0);
+            return;
+        }
+    }
+    distill_row<T, THREADS, NV, LSE>(a, row, z, g, c, first);
 }
 
 }  // namespace

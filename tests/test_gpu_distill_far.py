@@ -126,6 +126,12 @@ def test_long_rows_far_from_zero(ctx, vocab, dtype):
     compare(ctx, *far_rows(vocab, dtype, seed=vocab), 1.0, backward=False)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("vocab,t", [(1, 1.0), (50, 1.0), (700, 1e-9), (700, 0.01), (3001, 1.0), (9000, 0.5), (70000, 1.0), (140001, 1.0)])
+def test_both_directions_agree_far_from_zero(ctx, vocab, t, dtype):
+    compare(ctx, *far_rows(vocab, dtype, seed=vocab + 1), float(torch.tensor(t, dtype=torch.float32)))
+
+
 @pytest.mark.parametrize("t", [0.25, 1.0, 3.0])
 @pytest.mark.parametrize("vocab", [50, 70000])
 def test_teachers_far_from_zero(ctx, vocab, t):
