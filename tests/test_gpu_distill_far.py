@@ -144,3 +144,34 @@ def test_teachers_far_from_zero(ctx, vocab, t):
     top[12, 0], top[12, 1] = high, low
     top[13], top[13, 2] = -math.inf, -1e38
     compare(ctx, z[:16], ids[:16], top[:16], t, backward=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("vocab", [1003, 70001, 140003])
+def test_every_row_by_its_own_measure(ctx, vocab, dtype):
+    """Missing entries, places twice, masked places, rows without weight: each row's results are allowed what that row's sizes
+    allow, whatever else the batch holds."""
+    rows, k = 14, 24
+    g = torch.Generator().manual_seed(vocab)
+    z = (torch.randn(rows, vocab, generator=g) * 2.5).to(dtype)
+    top, ids = torch.topk(z.float() + 0.5 * torch.randn(rows, vocab, generator=g), k, 1)
+    ids = ids.int()
+    weight = torch.linspace(0.25, 2.0, rows)
+    weight[1] = 0.0
+    ids[2] = -1
+    ids[3, 5:] = -1
+    ids[4, ::2] = vocab
+    ids[4, 1] = -(2 ** 31)
+    top[5] = -math.inf
+    top[6, 3:] = -math.inf
+    ids[7, :] = ids[7, 0]
+    ids[8, 12:] = ids[8, :12]
+    z[9, : vocab // 2] = -math.inf
+    ids[9] = torch.arange(vocab - k, vocab)
+    z[10, vocab - 1] = torch.finfo(dtype).min
+    top[10, 0] = torch.finfo(torch.float32).min
+    z[11, k:] = torch.finfo(dtype).min
+    ids[11] = torch.arange(k)
+    z[12, ids[12, 0]] = -math.inf                    # the teacher says nothing there either
+    top[12, 0] = -math.inf
+    compare(ctx, z, ids, top, 1.0, weight)
