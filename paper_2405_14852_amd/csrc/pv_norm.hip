@@ -28,7 +28,7 @@ __device__ __forceinline__ float normed(float v, root rstd, float w, float &rest
     const float n = v * rstd.hi, dn = fmaf(v, rstd.lo, fmaf(v, rstd.hi, -n));
     const float p = n * w, dp = fmaf(dn, w, fmaf(n, w, -p)), s = p + dp;
     rest = dp - (s - p);
-    return dp == dp ? s : p;                                // (p infinite)
+    return fabsf(dp) < __builtin_inff() ? s : p;            // (p infinite: dp is so against it, or no number)
 }
 
 // One row's outputs from its stored sum v (a thread's eight values of it).  A code is that of the formula, not of a float32 that it
@@ -52,7 +52,7 @@ __device__ __forceinline__ void norm_out(const float (&v)[8], root rstd, const f
             for (int i = 0; i < 8; ++i) {
                 normed(v[i], rstd, w[i], rest);
                 const unsigned b = __float_as_uint(o[i]);
-                if (b << 13 == 0 && fabsf(rest) > 0.0f) o[i] = __uint_as_float((rest < 0.0f) == (o[i] < 0.0f) ? b + 1 : b - 1);
+                if (b << 13 == 0 && fabsf(rest) > 0.0f && fabsf(o[i]) < __builtin_inff()) o[i] = __uint_as_float((rest < 0.0f) == (o[i] < 0.0f) ? b + 1 : b - 1);
             }
         const unsigned scale = pv_mx_scale<FMT>(pv_mx_largest(o));
         const pv_u2 c = pv_mx_encode<FMT>(o, scale);
