@@ -307,23 +307,26 @@ __global__ __launch_bounds__(1024) void k_rms_norm_backward_long(const T *dy, co
     }
 }
 
-// dweight: the blocks' sums added in the order of the blocks, 32 threads a column for a part of them each
+// dweight: the blocks' sums added in the order of the blocks, 32 threads a column for a part of them each, and 32 columns at a time
 __global__ __launch_bounds__(1024) void k_sum_partials(const float *__restrict__ partial, int parts, int64_t cols,
                                                          float *__restrict__ out)
 {
     __shared__ float s[32][33];
     const int c = threadIdx.x & 31, e = threadIdx.x >> 5;
-    const int64_t col = (int64_t)blockIdx.x * 32 + c;
-    float sum = 0.0f;
-    if (col < cols)
+    for (int64_t first = (int64_t)blockIdx.x * 32; first < cols; first += (int64_t)gridDim.x * 32) {
+        const int64_t col = first + c;
+        float sum = 0.0f;
+        if (col < cols)
 #pragma unroll 8
-        for (int p = e * parts / 32; p < (e + 1) * parts / 32; ++p) sum += partial[(int64_t)p * cols + col];
-    s[e][c] = sum;
-    __syncthreads();
-    if (e == 0 && col < cols) {
+            for (int p = e * parts / 32; p < (e + 1) * parts / 32; ++p) sum += partial[(int64_t)p * cols + col];
+        s[e][c] = sum;
+        __syncthreads();
+        if (e == 0 && col < cols) {
 #pragma unroll
-        for (int i = 1; i < 32; ++i) sum += s[i][c];
-        out[col] = sum;
+            for (int i = 1; i < 32; ++i) sum += s[i][c];
+            out[col] = sum;
+        }
+        __syncthreads();
     }
 }
 
@@ -432,7 +435,9 @@ pv_status pv_launch_rms_norm_backward(pv_ctx *ctx, int64_t rows, int64_t cols, i
         return for_nv<4>(units, 512, [&](auto nv) { return launch(k_rms_norm_backward<T, 512, decltype(nv)::value>, 512); });
     });
     if (st != PV_OK || partial == dweight) return st;
-    hipLaunchKernelGGL(k_sum_partials, dim3((unsigned)((cols + 31) / 32)), dim3(1024), 0, ctx->stream, partial,
+    // (a launch's threads are counted in 32 bits: 2^21 blocks are half of that)
+    const int64_t sums = (cols + 31) / 32;
+    hipLaunchKernelGGL(k_sum_partials, dim3((unsigned)(sums < 1 << 21 ? sums : 1 << 21)), dim3(1024), 0, ctx->stream, partial,
                        (int)blocks, cols, dweight);
     PV_HIP(ctx, hipGetLastError());
     return PV_OK;

@@ -47,3 +47,29 @@ def test_outputs_beyond_float32_are_infinite(ctx, rows, cols, dtype):
     ref.check(y, want, torch.where(torch.isinf(want), 0.0, err) + ref.rounding(fine, dtype) * (1 + 2.0 ** -19))
     assert (scales[:, 1] == 255).all() and int(torch.count_nonzero(codes[:, 32:64])) == 0
     assert (scales[:, 0] != 255).all() and (scales[:, 2:] != 255).all()
+
+
+def test_gradients_of_more_columns_than_a_launch_counts_threads_for():
+    """32 threads a column: 2^27 columns are 2^32.  Two rows, so a column's sum has two terms; the row's dot product has 2^27, of which
+    a lane adds 2^17 one after the other."""
+    rows, cols = 2, (1 << 27) + 37
+    ctx = PVContext(0)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    dy, h = (torch.randn(rows, cols, generator=g, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+    weight = torch.rand(cols, generator=g, device=DEV) + 0.5
+    rstd = torch.tensor([0.75, 1.25], device=DEV)
+    dx, dweight = torch.full_like(dy, 7.0), torch.full((cols,), 7.0, device=DEV)
+    ctx.pv_rms_norm_backward(rows, cols, dy, None, h, weight, rstd, dx, dweight)
+    parts = [slice(at, min(at + (1 << 24), cols)) for at in range(0, cols, 1 << 24)]
+    r = rstd.double()[:, None]
+    terms = [dy[:, p].double() * weight[p].double() * h[:, p].double() * r for p in parts]
+    dot, size = (sum(f(t).sum(1, keepdim=True) for t in terms) / cols for f in (lambda t: t, torch.abs))
+    del terms
+    for p in parts:
+        d, n = dy[:, p].double(), h[:, p].double() * r
+        want = (d * n).sum(0)
+        assert ((dweight[p].double() - want).abs() <= 3 * 2.0 ** -24 * (d * n).abs().sum(0)).all()
+        want = r * (d * weight[p].double() - n * dot)
+        err = r * (n.abs() * size * (2 ** 17 + 64) * 2.0 ** -24 + ((d * weight[p].double()).abs() + (n * dot).abs()) * 4 * 2.0 ** -24)
+        assert ((dx[:, p].double() - want).abs() <= err + ref.rounding(want.abs() + err, torch.bfloat16)).all()
+    ctx.close()
