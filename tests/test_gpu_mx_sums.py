@@ -87,3 +87,22 @@ def test_every_product_is_of_the_codes_and_timed_once(ctx):
         ctx.pv_mx_product(200, 300, 512, "e4m3", xc, xs, wc, ws, y)
         assert ctx.pv_timing_read("mx_product")[1] == 1 and ctx.pv_timing_read("mx_convert")[1] == 0
         ctx.pv_timing_enable(False)
+
+
+@pytest.mark.parametrize("fmt", ["e2m1", "e4m3"])
+@pytest.mark.parametrize("tokens,out,inn", [(1, 33, 70), (40, 4100, 70), (130, 257, 300), (1100, 520, 1203)])
+def test_gradient_in_float16(ctx, tokens, out, inn, fmt):
+    g = torch.Generator().manual_seed(tokens)
+    x = torch.randn(tokens, inn, generator=g)
+    xc, xs = ref.quantize(x, fmt)
+    wc, ws = ref.quantize(torch.randn(out, inn, generator=g) * 0.02, "e2m1")
+    dy = torch.randn(tokens, out, generator=g).to(torch.bfloat16)
+    w, d = ref.decode(wc, ws, "e2m1", inn), dy.double()
+    dx, dw = torch.full((tokens, inn), 7.0, dtype=torch.float16, device=DEV), torch.full((out, inn), 7.0, device=DEV)
+    ctx.pv_mx_product_grads(tokens, out, inn, fmt, xc.to(DEV), xs.to(DEV), wc.to(DEV), ws.to(DEV), dy.to(DEV), dx, dw)
+    # an instruction adds 16 products of bfloat16 values to a float32 sum and may lose 2^-22 of the magnitudes in it
+    want, err = d @ w, (-(-out // 16) + 4) * 2.0 ** -22 * (d.abs() @ w.abs())
+    ref.check(dx, want, err + ref.rounding(want.abs() + err, torch.float16), "dX")
+    x = ref.decode(xc, xs, fmt, inn)
+    want, err = d.T @ x, (-(-tokens // 16) + 4) * 2.0 ** -22 * (d.abs().T @ x.abs())
+    ref.check(dw, want, err + ref.rounding(want, torch.float32), "dW")
