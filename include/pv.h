@@ -350,7 +350,9 @@ pv_status pv_mx_product_grads(pv_ctx *ctx, int64_t tokens, int64_t out_features,
 
 /* Root-mean-square norm with the residual's addition, per row of [rows, cols]:
  *   h = x + residual          rounded to `type` (residual NULL: h = x)
- *   rstd = (sum_i h_i^2 / cols + eps)^(-1/2)      f32, sum in f32, of the ROUNDED h
+ *   rstd = (sum_i h_i^2 / cols + eps)^(-1/2)      f32, of the ROUNDED h; the squares of eight values are added
+ *                                                 in f32 (with |h| above 2^62 they may leave it: rstd 0),
+ *                                                 those sums in double
  *   y_i = h_i * rstd * weight_i                   rounded once, rstd beyond f32
  * x, residual, h, y of `type`; weight f32 [cols].  Outputs, each NULL ok, at least one of them
  * given: h; y rounded to `type`; codes and scales, both or neither: y (not rounded to `type`
